@@ -296,6 +296,11 @@ def _logits(s, k, dt):
     return z.masked_fill(~seen[:, None], -math.inf)
 
 
+def _pair(hi, lo):
+    """The value that a hi + lo pair stands for: next to a tie of hi, lo alone is a matter of the last bit of the sum."""
+    return hi.float() + lo
+
+
 def _attention_value(s, k, v, dt):
     c = s["case"]
     batch, heads, kv_heads, head_dim, nq = c["batch"], c["heads"], c["kv_heads"], c["head_dim"], c["queries"]
@@ -360,8 +365,9 @@ def _run_plain(s):
     if c["kind"] == "attention":
         o, lse = _attention_value(s, _values(s["codes"][0]), _values(s["codes"][1]), f32)
         out = o.to(_dtype(c["out"]))
-        return dict(out=out, out_lo=(o - out.float()).to(torch.bfloat16) if c["out_lo"] else None,
-                    lse=lse if c["lse"] else None)
+        if c["out_lo"]:
+            out = _pair(out, (o - out.float()).to(torch.bfloat16))
+        return dict(out=out, lse=lse if c["lse"] else None)
     if c["kind"] == "score":
         s["scores"][..., :max(s["ctx"]) + s["n_local"]] += _score_value(s, _values(s["codes"][0]), f32)
         return s["scores"]
@@ -387,7 +393,7 @@ def _run_own(s):
     if c["kind"] == "attention":
         pkg.op_attention_kv4(s["q"], s["pool"], s["table"], s["n_ctx"], s["anc"], s["out"], c["queries"], c["q_local0"],
                              s["n_local"], c["queries"], c["heads"], c["head_dim"], out_lo=s["out_lo"], lse=s["lse"])
-        return dict(out=s["out"], out_lo=s["out_lo"], lse=s["lse"])
+        return dict(out=_pair(s["out"], s["out_lo"]) if c["out_lo"] else s["out"], lse=s["lse"])
     if c["kind"] == "score":
         pkg.op_kv4_score(s["q"], s["lse"], s["pool"], s["table"], s["n_ctx"], s["anc"], s["scores"], c["queries"],
                          c["q_local0"], s["n_local"], c["queries"], c["heads"], c["head_dim"], weight=s["weight"])
@@ -519,4 +525,4 @@ def exact(case, seed):
             sums[b, h // (heads // c["kv_heads"]), :p.shape[1]] += p.sum(0)
     if c["kind"] == "score":
         return sums
-    return dict(out=out, out_lo=None, lse=lse if c["lse"] else None)
+    return dict(out=out, lse=lse if c["lse"] else None)
