@@ -317,9 +317,82 @@ chimera_status chimera_op_attention(int dtype, int kv_split, int batch, int n_he
                                     int max_pages, const int32_t* n_ctx, const uint64_t* anc,
                                     void* out, void* out_lo, int ldo, int splits, void* cuda_stream);
 
+/* ---- 4-bit serving: weights and KV cache in 4 bits (stateless, like the ones above) ----
+ * The paper keeps weights and caches in 16 bits; these operators are a service of the
+ * library for serving the same models from a quarter of the bytes.  All are asynchronous on
+ * `cuda_stream` (NULL: default), take device pointers, and may overlap on several streams under
+ * chimera_op_linear's rule.  What a kernel meets on the device (a slot past the table: ECAPACITY;
+ * a block past the pool: EINVAL; such rows are skipped) is reported by chimera_op_sync.
+ *
+ * Y[M][N] (epilogue)= (X + X_lo)[M][K] . W^T with W[n][k] = scale[n][k / group] *
+ * (code[n][k] - zero[n][k / group]).  W: uint8 [N][K / 2], the code of column 2 j in the low
+ * nibble of byte j; scales: bf16 [N][ceil(K / group)]; zeros: uint8 0..15 of the same shape, or
+ * NULL for 8 everywhere.  group 32, 64 or 128; K a multiple of 32; the last group may be short.
+ * dtype 1: X, X_lo (optional) bf16; dtype 0: X fp32 (X_lo NULL), Y fp32.  X, X_lo and W
+ * 16-byte aligned, ldx a multiple of 16 bytes.  epi and out_f32 as in chimera_op_linear.  Code less
+ * zero is a whole number, so products are exact and are summed in fp32; a call's result
+ * does not depend on timing (no sum is taken in arrival order). */
+chimera_status chimera_op_linear_w4(int dtype, int epi, int out_f32, int M, int N, int K, int group, const void* X,
+                                    const void* X_lo, int ldx, const void* W, const void* scales, const void* zeros,
+                                    void* Y, int ldy, void* cuda_stream);
+
+/* The 4-bit paged cache.  pool: [n_blocks][kv_heads][16 head_dim + 128 bytes], 16-byte aligned,
+ * head_dim 64 or 128; a page holds 16 rows (K and V) of one head, each as head_dim codes 0..15 and a
+ * step and a base in bf16: base = bf16(min x), step = bf16((max x - min x) / 15; in fp32, times fp32(1 / 15)), code =
+ * clamp(rint((x - base) / step), 0, 15), and the row stands for base + step * code.  A row of equal
+ * values has step 0; a row holding a value that is not finite is kept as NaN.  page_table:
+ * int32 [batch][max_pages], shared by all heads.
+ *
+ * append rounds rows i < counts[b] (counts NULL: i < rows) of each sequence b into slots slot0[b] + i
+ * (device int32 [batch]); k, v: [batch * rows][ld], head g at column g * head_dim, fp32
+ * (dtype 0) or bf16 (1), keys already rotated.  read gives back what such rows stand for;
+ * rows past counts[b] are left as they are. */
+chimera_status chimera_op_kv4_append(int dtype, int batch, int rows, int kv_heads, int head_dim, const void* k, int ldk,
+                                     const void* v, int ldv, void* pool, int n_blocks, const int32_t* page_table,
+                                     int max_pages, const int32_t* slot0, const int32_t* counts, void* cuda_stream);
+chimera_status chimera_op_kv4_read(int dtype, int batch, int rows, int kv_heads, int head_dim, void* k, int ldk, void* v,
+                                   int ldv, const void* pool, int n_blocks, const int32_t* page_table, int max_pages,
+                                   const int32_t* slot0, const int32_t* counts, void* cuda_stream);
+
+/* Tree-masked attention over the 4-bit cache: chimera_op_attention's rows and masks (nq, q_local0,
+ * n_local, anc; anc may be NULL without local rows), with n_heads a multiple of kv_heads (head h
+ * reads kv head h / (n_heads / kv_heads)).  q fp32 (q_dtype 0) or bf16 (1); out fp32 (out_dtype 0) or
+ * bf16 (1) with an optional out_lo; lse (optional): fp32 [batch * q_rows][n_heads], natural log of each
+ * row's sum of exponentials (-inf for a row that sees nothing, whose output is zero).  splits: as in
+ * chimera_op_attention, at most 64; 0 lets the library choose.  A slot that no row may see
+ * is never part of a result, whatever its page holds. */
+chimera_status chimera_op_attention_kv4(int q_dtype, int out_dtype, int batch, int n_heads, int kv_heads, int head_dim, int nq,
+                                        int q_local0, int n_local, const void* q, int ldq, int q_rows, const void* pool,
+                                        int n_blocks, const int32_t* page_table, int max_pages, const int32_t* n_ctx,
+                                        const uint64_t* anc, void* out, void* out_lo, int ldo, float* lse, int splits,
+                                        void* cuda_stream);
+
+/* Attention weight drawn by each cached row: scores[b][g][slot] += sum over the query rows i and the heads
+ * h of kv head g of weight[b * q_rows + i] * exp(q . k / sqrt(head_dim) - lse[b * q_rows + i][h]) for
+ * every slot that the row may see (lse: chimera_op_attention_kv4's).  weight: fp32 [batch *
+ * q_rows] or NULL (1): e.g. 1 for the rows of an accepted path and 0 for the rest.  scores: fp32 [batch][kv_heads]
+ * [ld_scores]; sequences with more rows than ld_scores are ECAPACITY. */
+chimera_status chimera_op_kv4_score(int q_dtype, int batch, int n_heads, int kv_heads, int head_dim, int nq, int q_local0,
+                                    int n_local, const void* q, int ldq, int q_rows, const float* lse, const float* weight,
+                                    const void* pool, int n_blocks, const int32_t* page_table, int max_pages,
+                                    const int32_t* n_ctx, const uint64_t* anc, float* scores, int ld_scores,
+                                    void* cuda_stream);
+
+/* Eviction: of each sequence's n_ctx rows, every head keeps the `recent` newest and, of the rows before them,
+ * the budget - recent with the largest scores (ties: the lowest slot; a NaN ranks last), in slot
+ * order; a sequence of at most budget rows keeps all.  kept: int32 [batch][kv_heads][budget], the slots,
+ * -1 past the end; scores_out (same shape): their scores, 0 past the end; n_out: int32 [batch] =
+ * min(n_ctx, budget).  The kept rows are written to slots 0.. of the pages of dst_table (int32 [batch]
+ * [dst_pages], dst_pages >= ceil(budget / 16)), which must not be pages that page_table names
+ * for a sequence of the call: the move reads and writes at the same time. */
+chimera_status chimera_op_kv4_evict(int batch, int kv_heads, int head_dim, void* pool, int n_blocks, const int32_t* page_table,
+                                    int max_pages, const int32_t* n_ctx, const float* scores, int ld_scores, int budget,
+                                    int recent, const int32_t* dst_table, int dst_pages, int32_t* kept, float* scores_out,
+                                    int32_t* n_out, void* cuda_stream);
+
 /* Wait until `cuda_stream` (NULL: the default stream) is idle, then read and clear the
- * device error words of the stateless entry points (chimera_op_linear,
- * chimera_op_attention, chimera_op_linear_noalloc) on the current device: everything
+ * device error words of the stateless entry points (all chimera_op_* functions)
+ * on the current device: everything
  * their kernels flagged since the previous chimera_op_sync.  CHIMERA_ETIMEDOUT when a
  * bounded wait gave up (the outputs of those calls are undefined; the split counters
  * of the workspaces are reset, so later calls compute correctly again),

@@ -56,6 +56,9 @@ class Weights(ctypes.Structure):
 
 _lib = None
 
+_KV4_ROWS = [ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_int,
+             ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
+
 _SIGS = {
     "chimera_init": (ctypes.c_int, [ctypes.POINTER(Config), ctypes.POINTER(Weights), ctypes.c_void_p,
                                     ctypes.POINTER(ctypes.c_void_p)]),
@@ -92,6 +95,23 @@ _SIGS = {
                                                                  ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
                                                                  ctypes.c_void_p, ctypes.c_int, ctypes.c_int,
                                                                  ctypes.c_void_p]),
+    "chimera_op_linear_w4": (ctypes.c_int, [ctypes.c_int] * 7 + [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int] +
+                             [ctypes.c_void_p] * 4 + [ctypes.c_int, ctypes.c_void_p]),
+    "chimera_op_kv4_append": (ctypes.c_int, [ctypes.c_int] * 5 + _KV4_ROWS),
+    "chimera_op_kv4_read": (ctypes.c_int, [ctypes.c_int] * 5 + _KV4_ROWS),
+    "chimera_op_attention_kv4": (ctypes.c_int, [ctypes.c_int] * 9 + [ctypes.c_void_p, ctypes.c_int, ctypes.c_int,
+                                                                     ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p,
+                                                                     ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
+                                                                     ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int,
+                                                                     ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p]),
+    "chimera_op_kv4_score": (ctypes.c_int, [ctypes.c_int] * 8 + [ctypes.c_void_p, ctypes.c_int, ctypes.c_int,
+                                                                 ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                                                 ctypes.c_int, ctypes.c_void_p, ctypes.c_int,
+                                                                 ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                                                 ctypes.c_int, ctypes.c_void_p]),
+    "chimera_op_kv4_evict": (ctypes.c_int, [ctypes.c_int] * 3 + [ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_int,
+                                                                 ctypes.c_void_p, ctypes.c_void_p] + [ctypes.c_int] * 3 +
+                             [ctypes.c_void_p, ctypes.c_int] + [ctypes.c_void_p] * 4),
 }
 
 
@@ -374,6 +394,96 @@ def op_attention(q, pool, page_table, n_ctx, anc, out, nq, q_local0, n_local, q_
         raise ChimeraError(st, "chimera_op_attention")
 
 
+# ---- 4-bit serving ----
+def kv4_pool(n_blocks: int, kv_heads: int, head_dim: int, device="cuda"):
+    """An empty pool of the 4-bit cache: uint8 [n_blocks][kv_heads][bytes of a 16-row page]."""
+    import torch
+    return torch.zeros((n_blocks, kv_heads, 16 * head_dim + 128), dtype=torch.uint8, device=device)
+
+
+def w4_round(w, group: int = 128):
+    """Weights [N][K] rounded to nearest by groups of K columns, in the layout of op_linear_w4: packed codes
+    uint8 [N][K / 2], scales bf16 and zeros uint8 [N][ceil(K / group)].  Done once, when a model is loaded."""
+    import torch
+    n, k = w.shape
+    groups = -(-k // group)
+    x = torch.nn.functional.pad(w.float(), (0, groups * group - k)).view(n, groups, group)
+    lo, hi = x.amin(-1).clamp(max=0), x.amax(-1).clamp(min=0)
+    scale = ((hi - lo) / 15).clamp(min=1e-30).to(torch.bfloat16)
+    zero = torch.round(-lo / scale.float()).clamp(0, 15)
+    code = torch.round(x / scale.float()[..., None] + zero[..., None]).clamp(0, 15).to(torch.uint8).view(n, -1)[:, :k]
+    return (code[:, 0::2] | code[:, 1::2] << 4).contiguous(), scale, zero.to(torch.uint8)
+
+
+def _code(t) -> int:
+    return 0 if t.element_size() == 4 else 1
+
+
+def op_linear_w4(X, W, scales, Y, zeros=None, group: int = 128, epi: int = 0, out_f32: bool = False, X_lo=None, stream=None):
+    """Y (epilogue)= (X + X_lo) W^T with 4-bit weights through chimera_op_linear_w4: X, X_lo [M][K] (bf16; X fp32
+    without X_lo), W uint8 [N][K / 2], scales bf16 and zeros uint8 (or None: 8) [N][ceil(K / group)]."""
+    M, K = X.shape
+    st = load().chimera_op_linear_w4(_code(X), epi, int(out_f32), M, W.shape[0], K, group, _ptr(X), _ptr(X_lo), X.stride(0),
+                                     _ptr(W), _ptr(scales), _ptr(zeros), _ptr(Y), Y.stride(0), _stream_handle(stream))
+    if st != 0:
+        raise ChimeraError(st, "chimera_op_linear_w4")
+
+
+def op_kv4_append(k, v, pool, page_table, slot0, rows, head_dim, counts=None, stream=None):
+    """Round K and V rows to 4 bits into slots slot0[b] + i of each sequence, i < rows (or counts[b]), through
+    chimera_op_kv4_append.  k, v [batch * rows][kv_heads * head_dim] fp32 or bf16; pool from kv4_pool; page_table int32
+    [batch][max_pages]; slot0, counts int32 [batch] on the device."""
+    st = load().chimera_op_kv4_append(_code(k), page_table.shape[0], rows, pool.shape[1], head_dim, _ptr(k), k.stride(0),
+                                      _ptr(v), v.stride(0), _ptr(pool), pool.shape[0], _ptr(page_table),
+                                      page_table.shape[1], _ptr(slot0), _ptr(counts), _stream_handle(stream))
+    if st != 0:
+        raise ChimeraError(st, "chimera_op_kv4_append")
+
+
+def op_kv4_read(pool, page_table, slot0, rows, head_dim, k, v, counts=None, stream=None):
+    """What the cached rows stand for, into k and v (shapes as in op_kv4_append), through chimera_op_kv4_read."""
+    st = load().chimera_op_kv4_read(_code(k), page_table.shape[0], rows, pool.shape[1], head_dim, _ptr(k), k.stride(0),
+                                    _ptr(v), v.stride(0), _ptr(pool), pool.shape[0], _ptr(page_table), page_table.shape[1],
+                                    _ptr(slot0), _ptr(counts), _stream_handle(stream))
+    if st != 0:
+        raise ChimeraError(st, "chimera_op_kv4_read")
+
+
+def op_attention_kv4(q, pool, page_table, n_ctx, anc, out, nq, q_local0, n_local, q_rows, n_heads, head_dim, out_lo=None,
+                     lse=None, splits=0, stream=None):
+    """Tree-masked attention over the 4-bit cache through chimera_op_attention_kv4: op_attention's rows and masks,
+    q fp32 or bf16, out fp32 or bf16 (+ out_lo), lse fp32 [batch * q_rows][n_heads] (optional)."""
+    st = load().chimera_op_attention_kv4(_code(q), _code(out), n_ctx.shape[0], n_heads, pool.shape[1], head_dim, nq, q_local0,
+                                         n_local, _ptr(q), q.stride(0), q_rows, _ptr(pool), pool.shape[0],
+                                         _ptr(page_table), page_table.shape[1], _ptr(n_ctx), _ptr(anc), _ptr(out),
+                                         _ptr(out_lo), out.stride(0), _ptr(lse), splits, _stream_handle(stream))
+    if st != 0:
+        raise ChimeraError(st, "chimera_op_attention_kv4")
+
+
+def op_kv4_score(q, lse, pool, page_table, n_ctx, anc, scores, nq, q_local0, n_local, q_rows, n_heads, head_dim, weight=None,
+                 stream=None):
+    """Add the attention weight that each cached row draws to scores (fp32 [batch][kv_heads][slots]) through
+    chimera_op_kv4_score; lse from op_attention_kv4, weight fp32 [batch * q_rows] or None."""
+    st = load().chimera_op_kv4_score(_code(q), n_ctx.shape[0], n_heads, pool.shape[1], head_dim, nq, q_local0, n_local, _ptr(q),
+                                     q.stride(0), q_rows, _ptr(lse), _ptr(weight), _ptr(pool), pool.shape[0],
+                                     _ptr(page_table), page_table.shape[1], _ptr(n_ctx), _ptr(anc), _ptr(scores),
+                                     scores.stride(1), _stream_handle(stream))
+    if st != 0:
+        raise ChimeraError(st, "chimera_op_kv4_score")
+
+
+def op_kv4_evict(pool, page_table, n_ctx, scores, budget, recent, dst_table, kept, scores_out, n_out, head_dim, stream=None):
+    """Keep the `recent` newest rows and the best-scored of the others, `budget` in all, per head, in the pages of
+    dst_table, through chimera_op_kv4_evict (kept int32 and scores_out fp32 [batch][kv_heads][budget], n_out int32 [batch])."""
+    st = load().chimera_op_kv4_evict(n_ctx.shape[0], pool.shape[1], head_dim, _ptr(pool), pool.shape[0], _ptr(page_table),
+                                     page_table.shape[1], _ptr(n_ctx), _ptr(scores), scores.stride(1), budget, recent,
+                                     _ptr(dst_table), dst_table.shape[1], _ptr(kept), _ptr(scores_out), _ptr(n_out),
+                                     _stream_handle(stream))
+    if st != 0:
+        raise ChimeraError(st, "chimera_op_kv4_evict")
+
+
 def op_sync(stream=None):
     """Wait for the stateless entry points' work and raise what their kernels flagged
     on the device since the last call (ETIMEDOUT, EINVAL, ...)."""
@@ -392,4 +502,4 @@ def declared_symbols(header: str = HEADER) -> list[str]:
     import re
     src = open(header).read()
     src = re.sub(r"/\*.*?\*/", "", src, flags=re.S)
-    return sorted(set(re.findall(r"\b(chimera_[a-z_]+)\s*\(", src)))
+    return sorted(set(re.findall(r"\b(chimera_[a-z0-9_]+)\s*\(", src)))

@@ -7,7 +7,11 @@
 
 #include <atomic>
 
+struct __nv_bfloat16;
+
 namespace chimera {
+
+using bf16_raw = ::__nv_bfloat16;
 
 // ----------------------------------------------------------------------------
 // bf16 linear on tcgen05: Y[M][N] (epilogue) = X[M][K] . W[N][K]^T
@@ -327,5 +331,78 @@ cudaError_t argmax_rows(const float* logits, int V, int rows, int* out, cudaStre
 constexpr int TOPK_MAX_BLOCKS = 64;  // V <= 64 * 2048
 cudaError_t topk_rows(const float* logits, int V, int rows, int k, int* idx, float* val, int out_stride,
                       float* ws_v, int* ws_i, int* counters, cudaStream_t s);
+
+// ----------------------------------------------------------------------------
+// 4-bit weights and the 4-bit KV cache
+// ----------------------------------------------------------------------------
+// Y[M][N] (epilogue)= (X + X_lo)[M][K] . W^T, W[n][k] = scale[n][k / group] (code - zero[n][k / group]).
+struct W4Params {
+  const void* X;           // bf16, or fp32 (x_f32)
+  const bf16_raw* X_lo;    // optional (bf16 X)
+  int x_f32, ldx;
+  const unsigned char* W;  // [N][K / 2], code of 2 j in the low nibble of byte j
+  const bf16_raw* scale;   // [N][ceil(K / group)]
+  const unsigned char* zero;  // the same shape; null: 8
+  int group;               // 32, 64 or 128
+  int M, N, K;
+  int epi, out_f32;
+  void* Y;
+  int ldy;
+};
+cudaError_t linear_w4(const W4Params& p, cudaStream_t s);
+
+// The cache's pool: [n_blocks][G kv heads][kv4_page_bytes(hd)] (layout in kv4.cuh).
+struct Kv4Pool {
+  unsigned char* pool;
+  int n_blocks;
+  const int* table;  // [B][max_pages]
+  int max_pages;
+  int B, G, hd;
+  int* err;
+};
+// Rows i < counts[b] (all `rows` of them without counts) of sequence b, at slots slot0[b] + i:
+// k, v [b * rows + i][ld], head g at column g * hd, fp32 or bf16.
+cudaError_t kv4_append(const Kv4Pool& c, const void* k, const void* v, int f32, int ldk, int ldv, int rows,
+                       const int* slot0, const int* counts, cudaStream_t s);
+cudaError_t kv4_read(const Kv4Pool& c, void* k, void* v, int f32, int ldk, int ldv, int rows, const int* slot0,
+                     const int* counts, cudaStream_t s);
+
+struct Kv4AttnParams {
+  Kv4Pool c;
+  const void* q;      // rotated queries, row (b * q_rows + i), head h at column h * hd
+  int q_f32, ldq, q_rows, nq, q_local0, n_local, H;
+  const unsigned long long* anc;
+  const int* n_ctx;
+  float scale;
+  void* out;          // row (b * q_rows + i): fp32 or bf16
+  bf16_raw* out_lo;   // optional (bf16 out)
+  int out_f32, ldo;
+  float* lse;         // optional [B * q_rows][H]; the score kernel's input
+  int splits;
+  float* ws;
+  int* counters;      // [B * G * row tiles], zero between launches
+  // score: scores[(b * G + g) * ld_scores + slot] += sum over the rows of weight p
+  float* scores;
+  int ld_scores;
+  const float* weight;  // optional [B * q_rows]
+};
+int kv4_attn_row_tiles(int nq, int H, int G);
+int kv4_attn_splits(const Kv4AttnParams& p);
+size_t kv4_attn_ws_floats(const Kv4AttnParams& p);
+cudaError_t attention_kv4(const Kv4AttnParams& p, cudaStream_t s);
+cudaError_t kv4_score(const Kv4AttnParams& p, cudaStream_t s);
+
+struct Kv4EvictParams {
+  Kv4Pool c;
+  const int* n_ctx;
+  const float* scores;  // [B * G][ld_scores]
+  int ld_scores, budget, recent;
+  const int* dst_table;  // [B][dst_pages]
+  int dst_pages;
+  int* kept;            // [B * G][budget]
+  float* scores_out;    // [B * G][budget]
+  int* n_out;           // [B]
+};
+cudaError_t kv4_evict(const Kv4EvictParams& p, cudaStream_t s);
 
 }  // namespace chimera

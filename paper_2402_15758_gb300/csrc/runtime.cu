@@ -2039,6 +2039,8 @@ OpScratch* op_scratch(cudaStream_t s) {
   if (!sh.ready && !op_alloc(&sh, true)) return nullptr;
   return cudaStreamWaitEvent(s, sh.done, 0) == cudaSuccess ? &sh : nullptr;
 }
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+const OpScratch kNoScratch;
 bool op_done(const OpScratch* sc, cudaStream_t s) { return !sc->done || cudaEventRecord(sc->done, s) == cudaSuccess; }
 }  // namespace
 
@@ -2105,6 +2107,186 @@ chimera_status chimera_op_attention(int dtype, int kv_split, int batch, int n_he
   p.err = sc->err;
   p.nq_max = nq;
   const cudaError_t e = attention(p, dtype, s);
+  return op_done(sc, s) && e == cudaSuccess ? CHIMERA_OK : CHIMERA_ECUDA;
+}
+
+chimera_status chimera_op_linear_w4(int dtype, int epi, int out_f32, int M, int N, int K, int group, const void* X,
+                                    const void* X_lo, int ldx, const void* W, const void* scales, const void* zeros,
+                                    void* Y, int ldy, void* cuda_stream) {
+  const int wide = dtype == 0 ? 4 : 8;  // values in 16 bytes
+  if ((dtype != 0 && dtype != 1) || epi < 0 || epi > 2 || M < 1 || N < 1 || K < 32 || K % 32 != 0 ||
+      (group != 32 && group != 64 && group != 128) || !X || !W || !scales || !Y || ldx < K || ldx % wide != 0 || ldy < N ||
+      (dtype == 0 && X_lo) || M > 65535 * 8 || !aligned16(X) || !aligned16(X_lo) || !aligned16(W) ||
+      reinterpret_cast<uintptr_t>(scales) % 2 != 0)
+    return CHIMERA_EINVAL;
+  const int f32 = dtype == 0 || epi == EPI_RESID || out_f32;
+  if (reinterpret_cast<uintptr_t>(Y) % (f32 ? 4 : 2) != 0) return CHIMERA_EINVAL;
+  W4Params p{};
+  p.X = X;
+  p.X_lo = static_cast<const bf16_raw*>(X_lo);
+  p.x_f32 = dtype == 0;
+  p.ldx = ldx;
+  p.W = static_cast<const unsigned char*>(W);
+  p.scale = static_cast<const bf16_raw*>(scales);
+  p.zero = static_cast<const unsigned char*>(zeros);
+  p.group = group;
+  p.M = M;
+  p.N = N;
+  p.K = K;
+  p.epi = epi;
+  p.out_f32 = f32;
+  p.Y = Y;
+  p.ldy = ldy;
+  return linear_w4(p, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CHIMERA_OK : CHIMERA_ECUDA;
+}
+
+namespace {
+bool kv4_pool_ok(const void* pool, int n_blocks, const int32_t* table, int max_pages, int batch, int kv_heads, int head_dim) {
+  return pool && aligned16(pool) && n_blocks >= 1 && table && max_pages >= 1 && max_pages <= (1 << 26) && batch >= 1 &&
+         batch <= 65535 && kv_heads >= 1 && kv_heads <= 65535 && batch * static_cast<long long>(kv_heads) <= 65535 &&
+         (head_dim == 64 || head_dim == 128);
+}
+Kv4Pool kv4_pool(const void* pool, int n_blocks, const int32_t* table, int max_pages, int batch, int kv_heads, int head_dim,
+                 const OpScratch* sc) {
+  return Kv4Pool{static_cast<unsigned char*>(const_cast<void*>(pool)), n_blocks, table, max_pages, batch, kv_heads, head_dim,
+                 sc->err};
+}
+chimera_status kv4_rows(bool append, int dtype, int batch, int rows, int kv_heads, int head_dim, const void* k, int ldk,
+                        const void* v, int ldv, const void* pool, int n_blocks, const int32_t* table, int max_pages,
+                        const int32_t* slot0, const int32_t* counts, void* cuda_stream) {
+  const long long width = static_cast<long long>(kv_heads) * head_dim;
+  if ((dtype != 0 && dtype != 1) || !kv4_pool_ok(pool, n_blocks, table, max_pages, batch, kv_heads, head_dim) || rows < 0 ||
+      !k || !v || ldk < width || ldv < width || !slot0 || 2LL * batch * rows * kv_heads > (1LL << 33) ||
+      reinterpret_cast<uintptr_t>(k) % (dtype ? 2 : 4) != 0 || reinterpret_cast<uintptr_t>(v) % (dtype ? 2 : 4) != 0)
+    return CHIMERA_EINVAL;
+  if (rows == 0) return CHIMERA_OK;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  std::lock_guard<std::mutex> lk(g_op_mu);
+  OpScratch* sc = op_scratch(s);
+  if (!sc) return CHIMERA_ENOMEM;
+  const Kv4Pool c = kv4_pool(pool, n_blocks, table, max_pages, batch, kv_heads, head_dim, sc);
+  const cudaError_t e = append ? kv4_append(c, k, v, dtype == 0, ldk, ldv, rows, slot0, counts, s)
+                               : kv4_read(c, const_cast<void*>(k), const_cast<void*>(v), dtype == 0, ldk, ldv, rows, slot0, counts, s);
+  return op_done(sc, s) && e == cudaSuccess ? CHIMERA_OK : CHIMERA_ECUDA;
+}
+// What chimera_op_attention_kv4 and chimera_op_kv4_score share: their arguments, checked.
+bool kv4_queries(Kv4AttnParams* p, int dtype, int batch, int n_heads, int kv_heads, int head_dim, int nq, int q_local0, int n_local,
+                 const void* q, int ldq, int q_rows, const void* pool, int n_blocks, const int32_t* table, int max_pages,
+                 const int32_t* n_ctx, const uint64_t* anc) {
+  if ((dtype != 0 && dtype != 1) || !kv4_pool_ok(pool, n_blocks, table, max_pages, batch, kv_heads, head_dim) ||
+      n_heads < 1 || n_heads > 65535 || n_heads % kv_heads != 0 || nq < 1 || nq > 64 || n_local < 0 || n_local > 64 || q_local0 < 0 ||
+      q_local0 > 63 || !q || ldq < n_heads * static_cast<long long>(head_dim) || q_rows < nq || !n_ctx || (n_local > 0 && !anc) ||
+      reinterpret_cast<uintptr_t>(q) % (dtype ? 2 : 4) != 0)
+    return false;
+  p->q = q;
+  p->q_f32 = dtype == 0;
+  p->ldq = ldq;
+  p->q_rows = q_rows;
+  p->nq = nq;
+  p->q_local0 = q_local0;
+  p->n_local = n_local;
+  p->H = n_heads;
+  p->anc = reinterpret_cast<const unsigned long long*>(anc);
+  p->n_ctx = n_ctx;
+  p->scale = 1.0f / std::sqrt(static_cast<float>(head_dim));
+  return true;
+}
+}  // namespace
+
+chimera_status chimera_op_kv4_append(int dtype, int batch, int rows, int kv_heads, int head_dim, const void* k, int ldk,
+                                     const void* v, int ldv, void* pool, int n_blocks, const int32_t* page_table,
+                                     int max_pages, const int32_t* slot0, const int32_t* counts, void* cuda_stream) {
+  return kv4_rows(true, dtype, batch, rows, kv_heads, head_dim, k, ldk, v, ldv, pool, n_blocks, page_table, max_pages, slot0,
+                  counts, cuda_stream);
+}
+
+chimera_status chimera_op_kv4_read(int dtype, int batch, int rows, int kv_heads, int head_dim, void* k, int ldk, void* v,
+                                   int ldv, const void* pool, int n_blocks, const int32_t* page_table, int max_pages,
+                                   const int32_t* slot0, const int32_t* counts, void* cuda_stream) {
+  return kv4_rows(false, dtype, batch, rows, kv_heads, head_dim, k, ldk, v, ldv, pool, n_blocks, page_table, max_pages, slot0,
+                  counts, cuda_stream);
+}
+
+chimera_status chimera_op_attention_kv4(int q_dtype, int out_dtype, int batch, int n_heads, int kv_heads, int head_dim, int nq,
+                                        int q_local0, int n_local, const void* q, int ldq, int q_rows, const void* pool,
+                                        int n_blocks, const int32_t* page_table, int max_pages, const int32_t* n_ctx,
+                                        const uint64_t* anc, void* out, void* out_lo, int ldo, float* lse, int splits,
+                                        void* cuda_stream) {
+  Kv4AttnParams p{};
+  if (!kv4_queries(&p, q_dtype, batch, n_heads, kv_heads, head_dim, nq, q_local0, n_local, q, ldq, q_rows, pool, n_blocks,
+                   page_table, max_pages, n_ctx, anc) ||
+      (out_dtype != 0 && out_dtype != 1) || !out || (out_dtype == 0 && out_lo) || ldo < n_heads * head_dim || splits < 0 ||
+      splits > 64 || reinterpret_cast<uintptr_t>(out) % (out_dtype ? 2 : 4) != 0)
+    return CHIMERA_EINVAL;
+  p.c = kv4_pool(pool, n_blocks, page_table, max_pages, batch, kv_heads, head_dim, &kNoScratch);
+  p.out = out;
+  p.out_lo = static_cast<bf16_raw*>(out_lo);
+  p.out_f32 = out_dtype == 0;
+  p.ldo = ldo;
+  p.lse = lse;
+  p.splits = splits ? splits : kv4_attn_splits(p);
+  const long long tiles = static_cast<long long>(kv4_attn_row_tiles(nq, n_heads, kv_heads)) * batch * kv_heads;
+  if (tiles > OP_ATT_COUNTERS) return CHIMERA_EINVAL;
+  while (p.splits > 1 && kv4_attn_ws_floats(p) > OP_ATT_FLOATS) --p.splits;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  std::lock_guard<std::mutex> lk(g_op_mu);
+  OpScratch* sc = op_scratch(s);
+  if (!sc) return CHIMERA_ENOMEM;
+  p.c.err = sc->err;
+  p.ws = sc->att_ws;
+  p.counters = sc->att_cnt;
+  const cudaError_t e = attention_kv4(p, s);
+  return op_done(sc, s) && e == cudaSuccess ? CHIMERA_OK : CHIMERA_ECUDA;
+}
+
+chimera_status chimera_op_kv4_score(int q_dtype, int batch, int n_heads, int kv_heads, int head_dim, int nq, int q_local0,
+                                    int n_local, const void* q, int ldq, int q_rows, const float* lse, const float* weight,
+                                    const void* pool, int n_blocks, const int32_t* page_table, int max_pages,
+                                    const int32_t* n_ctx, const uint64_t* anc, float* scores, int ld_scores,
+                                    void* cuda_stream) {
+  Kv4AttnParams p{};
+  if (!kv4_queries(&p, q_dtype, batch, n_heads, kv_heads, head_dim, nq, q_local0, n_local, q, ldq, q_rows, pool, n_blocks,
+                   page_table, max_pages, n_ctx, anc) ||
+      !lse || !scores || ld_scores < 1)
+    return CHIMERA_EINVAL;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  std::lock_guard<std::mutex> lk(g_op_mu);
+  OpScratch* sc = op_scratch(s);
+  if (!sc) return CHIMERA_ENOMEM;
+  p.c = kv4_pool(pool, n_blocks, page_table, max_pages, batch, kv_heads, head_dim, sc);
+  p.lse = const_cast<float*>(lse);
+  p.weight = weight;
+  p.scores = scores;
+  p.ld_scores = ld_scores;
+  const cudaError_t e = kv4_score(p, s);
+  return op_done(sc, s) && e == cudaSuccess ? CHIMERA_OK : CHIMERA_ECUDA;
+}
+
+chimera_status chimera_op_kv4_evict(int batch, int kv_heads, int head_dim, void* pool, int n_blocks, const int32_t* page_table,
+                                    int max_pages, const int32_t* n_ctx, const float* scores, int ld_scores, int budget,
+                                    int recent, const int32_t* dst_table, int dst_pages, int32_t* kept, float* scores_out,
+                                    int32_t* n_out, void* cuda_stream) {
+  if (!kv4_pool_ok(pool, n_blocks, page_table, max_pages, batch, kv_heads, head_dim) || !n_ctx || !scores || ld_scores < 1 ||
+      budget < 1 || recent < 0 || recent > budget || !dst_table || dst_pages < 1 || (budget + 15) / 16 > dst_pages || !kept ||
+      !scores_out || !n_out)
+    return CHIMERA_EINVAL;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  std::lock_guard<std::mutex> lk(g_op_mu);
+  OpScratch* sc = op_scratch(s);
+  if (!sc) return CHIMERA_ENOMEM;
+  Kv4EvictParams p{};
+  p.c = kv4_pool(pool, n_blocks, page_table, max_pages, batch, kv_heads, head_dim, sc);
+  p.n_ctx = n_ctx;
+  p.scores = scores;
+  p.ld_scores = ld_scores;
+  p.budget = budget;
+  p.recent = recent;
+  p.dst_table = dst_table;
+  p.dst_pages = dst_pages;
+  p.kept = kept;
+  p.scores_out = scores_out;
+  p.n_out = n_out;
+  const cudaError_t e = kv4_evict(p, s);
   return op_done(sc, s) && e == cudaSuccess ? CHIMERA_OK : CHIMERA_ECUDA;
 }
 
