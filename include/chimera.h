@@ -329,7 +329,7 @@ chimera_status chimera_op_attention(int dtype, int kv_split, int batch, int n_he
  * nibble of byte j; scales: bf16 [N][ceil(K / group)]; zeros: uint8 0..15 of the same shape, or
  * NULL for 8 everywhere.  group 32, 64 or 128; K a multiple of 32; the last group may be short.
  * dtype 1: X, X_lo (optional) bf16; dtype 0: X fp32 (X_lo NULL), Y fp32.  X, X_lo and W
- * 16-byte aligned, ldx a multiple of 16 bytes.  epi and out_f32 as in chimera_op_linear.  Code less
+ * 16-byte aligned like the scales and zeros, ldx a multiple of 16 bytes.  epi and out_f32 as in chimera_op_linear.  Code less
  * zero is a whole number, so products are exact and are summed in fp32; a call's result
  * does not depend on timing (no sum is taken in arrival order). */
 chimera_status chimera_op_linear_w4(int dtype, int epi, int out_f32, int M, int N, int K, int group, const void* X,

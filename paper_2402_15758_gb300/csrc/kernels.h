@@ -348,6 +348,9 @@ struct W4Params {
   int epi, out_f32;
   void* Y;
   int ldy;
+  int* err;
+  float* ws;               // scratch of linear_w4_ws_floats() floats
+  int* counters;           // tc_max_tiles(), zero between launches
 };
 cudaError_t linear_w4(const W4Params& p, cudaStream_t s);
 

@@ -53,18 +53,29 @@ inline int kv4_page_bytes(int hd) { return KV4_ROWS * hd + 128; }
 __device__ __forceinline__ float kv4_step(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float kv4_base(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// The eight codes of a word less 8, exact in fp16: pairs of nibbles (0,4), (1,5), (2,6), (3,7).
-// 0x6400 | c is 1024 + c, and 0x6400 | (c << 4) is 1024 + 16 c.
+// (x & mask) | bits in one instruction (the compiler makes two of it when both are constants).
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(x), "r"(mask), "r"(bits));
+  return r;
+}
+// The nibbles of a word as fp16 pairs (0,4), (1,5), (2,6), (3,7): 1024 + c in pairs 0 and 2, 1024 + 16 c in
+// 1 and 3 (ten bits of mantissa hold a nibble at either place).
+__device__ __forceinline__ void nibbles_f16(uint32_t w, uint32_t (&u)[4]) {
+  const uint32_t h = w >> 8;
+  u[0] = and_or(w, 0x000f000fu, 0x64006400u);
+  u[1] = and_or(w, 0x00f000f0u, 0x64006400u);
+  u[2] = and_or(h, 0x000f000fu, 0x64006400u);
+  u[3] = and_or(h, 0x00f000f0u, 0x64006400u);
+}
+
+// The eight codes of a word less 8, exact in fp16, paired as above.
 __device__ __forceinline__ void kv4_codes(uint32_t w, uint32_t (&r)[4]) {
   const __half2 off = __halves2half2(__ushort_as_half(0x6408), __ushort_as_half(0x6408));    // 1032
   const __half2 sixteenth = __halves2half2(__ushort_as_half(0x2c00), __ushort_as_half(0x2c00));
   const __half2 off16 = __halves2half2(__ushort_as_half(0xd480), __ushort_as_half(0xd480));  // -72
   uint32_t u[4];
-  u[0] = (w & 0x000f000fu) | 0x64006400u;
-  u[1] = (w & 0x00f000f0u) | 0x64006400u;
-  const uint32_t h = w >> 8;
-  u[2] = (h & 0x000f000fu) | 0x64006400u;
-  u[3] = (h & 0x00f000f0u) | 0x64006400u;
+  nibbles_f16(w, u);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     __half2 x = *reinterpret_cast<__half2*>(&u[i]);
@@ -80,6 +91,15 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// The same with d = A B.
+__device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                              uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 
 // Two fp32 values as a pair of fp16 and the pair of what that rounding left.

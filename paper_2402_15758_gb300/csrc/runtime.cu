@@ -2117,7 +2117,7 @@ chimera_status chimera_op_linear_w4(int dtype, int epi, int out_f32, int M, int 
   if ((dtype != 0 && dtype != 1) || epi < 0 || epi > 2 || M < 1 || N < 1 || K < 32 || K % 32 != 0 ||
       (group != 32 && group != 64 && group != 128) || !X || !W || !scales || !Y || ldx < K || ldx % wide != 0 || ldy < N ||
       (dtype == 0 && X_lo) || M > 65535 * 8 || !aligned16(X) || !aligned16(X_lo) || !aligned16(W) ||
-      reinterpret_cast<uintptr_t>(scales) % 2 != 0)
+      !aligned16(scales) || !aligned16(zeros))
     return CHIMERA_EINVAL;
   const int f32 = dtype == 0 || epi == EPI_RESID || out_f32;
   if (reinterpret_cast<uintptr_t>(Y) % (f32 ? 4 : 2) != 0) return CHIMERA_EINVAL;
@@ -2137,7 +2137,15 @@ chimera_status chimera_op_linear_w4(int dtype, int epi, int out_f32, int M, int 
   p.out_f32 = f32;
   p.Y = Y;
   p.ldy = ldy;
-  return linear_w4(p, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CHIMERA_OK : CHIMERA_ECUDA;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  std::lock_guard<std::mutex> lk(g_op_mu);
+  OpScratch* sc = op_scratch(s);
+  if (!sc) return CHIMERA_ENOMEM;
+  p.err = sc->err;
+  p.ws = sc->lin_ws;
+  p.counters = sc->lin_cnt;
+  const cudaError_t e = linear_w4(p, s);
+  return op_done(sc, s) && e == cudaSuccess ? CHIMERA_OK : CHIMERA_ECUDA;
 }
 
 namespace {
