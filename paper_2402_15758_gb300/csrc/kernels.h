@@ -349,10 +349,14 @@ struct W4Params {
   void* Y;
   int ldy;
   int* err;
-  float* ws;               // scratch of linear_w4_ws_floats() floats
+  float* ws;               // parts of tiles: tc_ws_floats(256) floats
   int* counters;           // tc_max_tiles(), zero between launches
+  void* scratch;           // the activations as fp16
+  size_t scratch_bytes;
 };
 cudaError_t linear_w4(const W4Params& p, cudaStream_t s);
+// The kernel for many tokens (linear_w4_tc.cu).
+cudaError_t linear_w4_many(const W4Params& p, cudaStream_t s);
 
 // The cache's pool: [n_blocks][G kv heads][kv4_page_bytes(hd)] (layout in kv4.cuh).
 struct Kv4Pool {
