@@ -350,7 +350,6 @@ struct W4Params {
   int ldy;
   int* err;
   float* ws;               // parts of tiles: tc_ws_floats(256) floats
-  int* counters;           // tc_max_tiles(), zero between launches
   void* scratch;           // the activations as fp16
   size_t scratch_bytes;
 };

@@ -2143,7 +2143,6 @@ chimera_status chimera_op_linear_w4(int dtype, int epi, int out_f32, int M, int 
   if (!sc) return CHIMERA_ENOMEM;
   p.err = sc->err;
   p.ws = sc->lin_ws;
-  p.counters = sc->lin_cnt;
   p.scratch = sc->att_ws;
   p.scratch_bytes = OP_ATT_FLOATS * sizeof(float);
   const cudaError_t e = linear_w4(p, s);
