@@ -14,6 +14,8 @@
 // have no bank conflicts by the page's layout.  Rows of all heads of a group and all queries are one
 // list, cut into tiles of 8; the keys of a tile are cut into `splits` ranges, whose results
 // the last block to finish merges in their order (no sum depends on who comes first).
+#include <algorithm>
+
 #include "kernels.h"
 #include "kv4.cuh"
 #include "launch.cuh"
@@ -21,7 +23,7 @@
 namespace chimera {
 namespace {
 
-constexpr int WARPS = 8, STAGES = 4, ROWS = 8;
+constexpr int WARPS = 4;
 constexpr float NONE = -1e30f;  // the reference of a row that has seen no key
 constexpr float LOG2E = 1.4426950408889634f;
 // Probabilities are taken relative to a reference 2^11 below a row's maximum, which is raised when a
@@ -30,16 +32,12 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr float BELOW = 11.f, SLACK = 15.f;
 constexpr unsigned long long WAIT_NS = 2000000000ull;
 
-template <int HD>
-struct Smem {
-  static constexpr int PAGE = Kv4<HD>::BYTES;
-  static constexpr int RING = STAGES * PAGE;  // of a warp; later its 8 x HD sums
-  static constexpr int BARS = WARPS * RING;
-  static constexpr int ML = BARS + WARPS * STAGES * 8;  // maximum and sum of each warp's rows
-  static constexpr int BYTES = ML + WARPS * ROWS * 8;
-  static_assert(RING >= ROWS * HD * 4, "the sums reuse the ring");
-};
-
+// 2^x, relative error 2^-22; results below 2^-126 are 0.
+__device__ __forceinline__ float pow2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ float quad_sum(float x) {
   x += __shfl_xor_sync(0xffffffffu, x, 1);
   return x + __shfl_xor_sync(0xffffffffu, x, 2);
@@ -49,35 +47,66 @@ __device__ __forceinline__ float quad_max(float x) {
   return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
 }
 
-// A fragments of 8 query rows: thread (r, t) = (lane / 4, lane % 4) holds channels
-// [t HD/4, (t + 1) HD/4) of row r, paired as the K words' nibbles are.  scale: by what q . c'
-// is multiplied to give base-2 logits; sum: of the row, times the same without the power of two.
+// 2^(4 - floor(log2 top)), at most 2^126 (1 for 0 and what is not finite).
+__device__ __forceinline__ float row_scale(float top) {
+  const int e = static_cast<int>(__float_as_uint(top) >> 23);
+  return __uint_as_float(static_cast<uint32_t>(e == 0 || e == 255 ? 127 : min(258 - e, 253)) << 23);
+}
+
+// HD / 4 consecutive values, 16 bytes at a time where they are aligned.
+template <int HD>
+__device__ __forceinline__ void load_quarter(const float* q, float (&x)[HD / 4]) {
+  if ((reinterpret_cast<uintptr_t>(q) & 15) == 0) {
+#pragma unroll
+    for (int i = 0; i < HD / 16; ++i) *reinterpret_cast<float4*>(x + 4 * i) = reinterpret_cast<const float4*>(q)[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < HD / 4; ++i) x[i] = q[i];
+  }
+}
+template <int HD>
+__device__ __forceinline__ void load_quarter(const bf16* q, float (&x)[HD / 4]) {
+#pragma unroll
+  for (int i = 0; i < HD / 4; ++i) x[i] = __bfloat162float(q[i]);
+}
+
+// A thread's quarter of a query row (channels [t HD/4, (t + 1) HD/4), t = lane % 4).  scale: by what the products of
+// the scaled row are multiplied to give base-2 logits; sum: of the row, times the same without the power of two.
+template <int HD, typename TQ>
+__device__ __forceinline__ void load_row(const TQ* q, bool there, float softmax_scale, float (&x)[HD / 4], float& scale, float& sum) {
+  float top = 0.f, s[4] = {};
+  if (there) load_quarter<HD>(q, x);
+#pragma unroll
+  for (int i = 0; i < HD / 4; ++i) {
+    x[i] = there ? x[i] : 0.f;
+    top = fmaxf(top, fabsf(x[i]));
+    s[i % 4] += x[i];
+  }
+  const float up = row_scale(quad_max(top));
+  scale = softmax_scale / up;
+  sum = quad_sum((s[0] + s[1]) + (s[2] + s[3])) * softmax_scale;
+#pragma unroll
+  for (int i = 0; i < HD / 4; ++i) x[i] *= up;
+}
+
+// A fragments of 8 query rows, hi and lo terms (the 16 rows of a product): thread (r, t) holds row r, paired
+// as the K words' nibbles are.
 template <int HD, typename TQ>
 __device__ __forceinline__ void load_rows(const TQ* q, bool there, float softmax_scale, uint32_t (&f)[HD / 16][4], float& scale,
                                           float& sum) {
-  constexpr int C = HD / 4;
-  float x[C];
-  float top = 0.f, s = 0.f;
-#pragma unroll
-  for (int i = 0; i < C; ++i) {
-    x[i] = there ? to_f<TQ>(q[i]) : 0.f;
-    top = fmaxf(top, fabsf(x[i]));
-    s += x[i];
-  }
-  top = quad_max(top);
-  s = quad_sum(s);
-  // 2^(4 - floor(log2 top)), at most 2^126
-  const int e = static_cast<int>(__float_as_uint(top) >> 23);
-  const int k = e == 0 || e == 255 ? 127 : min(254 - e + 4, 253);
-  const float up = __uint_as_float(static_cast<uint32_t>(k) << 23);
-  scale = softmax_scale / up;
-  sum = s * softmax_scale;
+  float x[HD / 4];
+  load_row<HD, TQ>(q, there, softmax_scale, x, scale, sum);
 #pragma unroll
   for (int j = 0; j < HD / 16; ++j) {
     const int at = j / 2 * 8 + 2 * (j & 1);
-    split_f16(x[at] * up, x[at + 4] * up, f[j][0], f[j][1]);
-    split_f16(x[at + 1] * up, x[at + 5] * up, f[j][2], f[j][3]);
+    split_f16(x[at], x[at + 4], f[j][0], f[j][1]);
+    split_f16(x[at + 1], x[at + 5], f[j][2], f[j][3]);
   }
+}
+
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
 }
 
 // q . c' of 8 rows (hi and lo) with the 16 keys of a page: s0 keys 2t, 2t + 1, s1 keys 8 + those.
@@ -95,6 +124,8 @@ __device__ __forceinline__ void page_dots(const unsigned char* page, const uint3
     *reinterpret_cast<uint2*>(a) = *reinterpret_cast<const uint2*>(k0);
     *reinterpret_cast<uint2*>(b) = *reinterpret_cast<const uint2*>(k1);
   }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s0[i] = s1[i] = 0.f;
 #pragma unroll
   for (int w = 0; w < NW; ++w) {
     uint32_t u[4];
@@ -159,86 +190,150 @@ __device__ __forceinline__ void store_out(const Kv4AttnParams& p, size_t at, T v
   store_act(static_cast<bf16*>(p.out), reinterpret_cast<bf16*>(p.out_lo), at, v);
 }
 
-template <int HD, typename TQ>
-__global__ void __launch_bounds__(WARPS * 32) attn_kv4_kernel(const __grid_constant__ Kv4AttnParams p) {
+// Writes a merged row (of the rows of a sequence and kv head): lane l has columns l, l + 32, ..
+template <int HD>
+__device__ __forceinline__ void store_row(const Kv4AttnParams& p, int bg, int row, int lane, float M, float L, const float (&acc)[HD / 32]) {
+  const int group = p.H / p.c.G, head = bg % p.c.G * group + row % group;
+  const size_t out = static_cast<size_t>(bg / p.c.G) * p.q_rows + row / group;
+  const float inv = L == 0.f ? 0.f : 1.f / L;  // a row that sees nothing gives zeros
+#pragma unroll
+  for (int i = 0; i < HD / 32; ++i) store_out(p, out * p.ldo + head * HD + lane + 32 * i, acc[i] * inv);
+  if (p.lse && lane == 0) p.lse[out * p.H + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+}
+
+// What a block's warps do: RTW tiles of rows times WARPS / RTW slices of the pages.  PRECISE: tiles of 8 rows in two
+// terms; else 16 rows in one (2^-12 of a query and of a weight, a tenth of the rounding of a bf16 result).
+template <int HD, bool PRECISE, int RTW>
+struct Shape {
+  static constexpr int TILE = PRECISE ? 8 : 16, ROWS = TILE * RTW, SLICES = WARPS / RTW;
+  static constexpr int STAGES = 6;  // pages of a slice: three pairs
+  static constexpr int RING = STAGES * Kv4<HD>::BYTES;
+  static constexpr int SUMS = WARPS * TILE * HD * 4;  // over the rings
+  static constexpr int BARS = SLICES * RING > SUMS ? SLICES * RING : SUMS;
+  static constexpr int ML = BARS + SLICES * STAGES * 16;  // reference and sum of each warp's rows
+  static constexpr int BYTES = ML + WARPS * TILE * 8;
+};
+
+template <int HD, typename TQ, bool PRECISE, int RTW>
+__global__ void __launch_bounds__(WARPS * 32, 3) attn_kv4_kernel(const __grid_constant__ Kv4AttnParams p) {
   extern __shared__ __align__(128) unsigned char smem[];
-  using S = Smem<HD>;
+  using S = Shape<HD, PRECISE, RTW>;
   using P = Kv4<HD>;
-  __shared__ int sh_abort, sh_last;
+  constexpr int TILE = S::TILE, NR = PRECISE ? 1 : 2, STAGES = S::STAGES;  // NR: rows of a thread
+  __shared__ int sh_abort;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31, r = lane / 4, t = lane & 3;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::BARS) + warp * STAGES;
-  unsigned char* ring = smem + warp * S::RING;
+  const int rt = warp % RTW, slice = warp / RTW;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::BARS) + slice * 2 * STAGES;
+  uint64_t* empty = full + STAGES;
+  unsigned char* ring = smem + slice * S::RING;
   if (tid == 0) sh_abort = 0;
-  if (lane == 0) {
-    for (int i = 0; i < STAGES; ++i) mbar_init(bars + i, 1);
+  if (lane == 0 && rt == 0) {
+    for (int i = 0; i < STAGES; ++i) {
+      mbar_init(full + i, 1);
+      mbar_init(empty + i, RTW);
+    }
     mbar_fence_init();
   }
   __syncthreads();
   pdl_wait();
   pdl_trigger();
 
-  const int group = p.H / p.c.G, n_rows = p.nq * group, tiles = (n_rows + ROWS - 1) / ROWS;
-  const int bg = blockIdx.y / tiles, tile = blockIdx.y % tiles, b = bg / p.c.G, g = bg % p.c.G;
-  Seen seen = what_is_seen(p, b);
-  const int row = tile * ROWS + r;
-  const bool there = row < n_rows;
-  const int qi = there ? row / group : 0, head = g * group + (there ? row % group : 0);
-  if (there && p.n_local) seen.local = p.anc[p.q_local0 + qi];
+  const int group = p.H / p.c.G, n_rows = p.nq * group, blocks = (n_rows + S::ROWS - 1) / S::ROWS;
+  const int bg = blockIdx.y / blocks, row0 = blockIdx.y % blocks * S::ROWS, b = bg / p.c.G, g = bg % p.c.G;
+  const Seen all = what_is_seen(p, b);
 
-  // the pages of this block, dealt to its warps in turn
-  const int pages = (seen.total + KV4_ROWS - 1) / KV4_ROWS;
+  // the pages of this block, dealt to its slices in turn
+  const int pages = (all.total + KV4_ROWS - 1) / KV4_ROWS;
   const int split = blockIdx.x, splits = gridDim.x;
   const int p0 = static_cast<int>(static_cast<long long>(pages) * split / splits);
   const int p1 = static_cast<int>(static_cast<long long>(pages) * (split + 1) / splits);
-  const int mine = max(0, (p1 - p0 - warp + WARPS - 1) / WARPS);
+  const int mine = max(0, (p1 - p0 - slice + S::SLICES - 1) / S::SLICES);
   const int* table = p.c.table + static_cast<size_t>(b) * p.c.max_pages;
-  auto request = [&](int k) {  // lane 0: page p0 + warp + k WARPS into its place of the ring
-    const int block = block_of(p, table, p0 + warp + k * WARPS);
-    uint64_t* bar = bars + k % STAGES;
-    mbar_arrive_expect_tx(bar, P::BYTES);
-    bulk_load(ring + k % STAGES * P::BYTES, p.c.pool + (static_cast<size_t>(block) * p.c.G + g) * P::BYTES, P::BYTES, bar);
+  int asked = 0;
+  auto request = [&]() {  // one lane: the next page into its place of the ring
+    const int block = block_of(p, table, p0 + slice + asked * S::SLICES), stage = asked % STAGES;
+    mbar_arrive_expect_tx(full + stage, P::BYTES);
+    bulk_load(ring + stage * P::BYTES, p.c.pool + (static_cast<size_t>(block) * p.c.G + g) * P::BYTES, P::BYTES, full + stage);
+    ++asked;
   };
-  if (lane == 0)
-    for (int k = 0; k < min(mine, STAGES); ++k) request(k);
+  if (lane == 0 && rt == 0)
+    while (asked < min(mine, STAGES - 2)) request();
 
   uint32_t qf[HD / 16][4];
-  float q_scale, q_sum;
-  load_rows<HD, TQ>(static_cast<const TQ*>(p.q) + (static_cast<size_t>(b) * p.q_rows + qi) * p.ldq + head * HD + t * (HD / 4), there,
-                    p.scale * LOG2E, qf, q_scale, q_sum);
+  float q_scale[NR], q_sum[NR];
+  unsigned long long local[NR];
+#pragma unroll
+  for (int i = 0; i < NR; ++i) {
+    const int row = row0 + rt * TILE + r + 8 * i;
+    const bool there = row < n_rows;
+    const int qi = there ? row / group : 0, head = g * group + (there ? row % group : 0);
+    local[i] = there && p.n_local ? p.anc[p.q_local0 + qi] : 0;
+    const TQ* q = static_cast<const TQ*>(p.q) + (static_cast<size_t>(b) * p.q_rows + qi) * p.ldq + head * HD + t * (HD / 4);
+    if constexpr (PRECISE) {
+      load_rows<HD, TQ>(q, there, p.scale * LOG2E, qf, q_scale[i], q_sum[i]);
+    } else {
+      float x[HD / 4];
+      load_row<HD, TQ>(q, there, p.scale * LOG2E, x, q_scale[i], q_sum[i]);
+#pragma unroll
+      for (int j = 0; j < HD / 16; ++j) {
+        const int at = j / 2 * 8 + 2 * (j & 1);
+        qf[j][i] = pack_f16(x[at], x[at + 4]);
+        qf[j][2 + i] = pack_f16(x[at + 1], x[at + 5]);
+      }
+    }
+  }
 
   float o[HD / 8][4] = {};
-  float m = NONE, l = 0.f, bs = 0.f;     // l and bs: this thread's keys alone
+  float m[NR], l[NR], bs[NR];  // l and bs: this thread's keys alone
+#pragma unroll
+  for (int i = 0; i < NR; ++i) m[i] = NONE, l[i] = bs[i] = 0.f;
   float top = 0x1p-126f, inv_top = 0x1p126f;  // power of two above every V step so far
-  for (int k = 0; k < mine; ++k) {
-    if (!mbar_wait_warp(bars + k % STAGES, k / STAGES & 1, &sh_abort, WAIT_NS)) {
-      // pages still in flight land before the block leaves
-      for (int i = k; i < min(mine, k + STAGES); ++i) mbar_wait_plain(bars + i % STAGES, i / STAGES & 1, WAIT_NS);
+  int stage = 0;
+  uint32_t phase = 0;
+  for (int k = 0; k < mine; k += 2) {
+    const bool two = k + 1 < mine;
+    if (!mbar_wait_warp(full + stage, phase, &sh_abort, WAIT_NS) || (two && !mbar_wait_warp(full + stage + 1, phase, &sh_abort, WAIT_NS))) {
       if (lane == 0) atomicOr(p.c.err, ERR_TIMEOUT);
       break;
     }
-    const unsigned char* page = ring + k % STAGES * P::BYTES;
-    float s0[4] = {}, s1[4] = {};
-    page_dots<HD>(page, qf, r, t, s0, s1);
-    float step[4], base[4], z[4];
-    key_scales(page + P::KS, t, step, base);
-    z[0] = fmaf(step[0] * q_scale, s0[0] + s0[2], base[0] * q_sum);
-    z[1] = fmaf(step[1] * q_scale, s0[1] + s0[3], base[1] * q_sum);
-    z[2] = fmaf(step[2] * q_scale, s1[0] + s1[2], base[2] * q_sum);
-    z[3] = fmaf(step[3] * q_scale, s1[1] + s1[3], base[3] * q_sum);
-    key_scales(page + P::VS, t, step, base);
-    const int slot0 = (p0 + warp + k * WARPS) * KV4_ROWS;
-    if (slot0 + KV4_ROWS > seen.n) {  // a hidden key counts nothing, whatever its codes and steps are
+    const unsigned char* page[2] = {ring + stage * P::BYTES, ring + (stage + (two ? 1 : 0)) * P::BYTES};
+    float z[2][NR][4], step[2][4], base[2][4];
+    float zmax[NR], smax = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (!seen(slot0 + 2 * t + (i & 1) + 8 * (i >> 1))) {
-          z[i] = -INFINITY;
-          step[i] = 0.f;
-          base[i] = 0.f;
+    for (int i = 0; i < NR; ++i) zmax[i] = -INFINITY;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float s0[4], s1[4];
+      page_dots<HD>(page[h], qf, r, t, s0, s1);
+      key_scales(page[h] + P::KS, t, step[h], base[h]);
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        const float d[4] = {PRECISE ? s0[0] + s0[2] : s0[2 * i], PRECISE ? s0[1] + s0[3] : s0[2 * i + 1],
+                            PRECISE ? s1[0] + s1[2] : s1[2 * i], PRECISE ? s1[1] + s1[3] : s1[2 * i + 1]};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) z[h][i][j] = fmaf(step[h][j] * q_scale[i], d[j], base[h][j] * q_sum[i]);
+      }
+      key_scales(page[h] + P::VS, t, step[h], base[h]);
+      const int slot0 = (p0 + slice + (k + h) * S::SLICES) * KV4_ROWS;
+      if (slot0 + KV4_ROWS > all.n || (h && !two)) {  // a hidden key counts nothing, whatever its codes and steps are
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int slot = slot0 + 2 * t + (j & 1) + 8 * (j >> 1);
+          const bool held = slot < all.total && !(h && !two);
+          if (!held) step[h][j] = base[h][j] = 0.f;
+#pragma unroll
+          for (int i = 0; i < NR; ++i)
+            if (!held || (slot >= all.n && !(local[i] >> (slot - all.n) & 1))) z[h][i][j] = -INFINITY;
         }
+      }
+#pragma unroll
+      for (int i = 0; i < NR; ++i) zmax[i] = fmaxf(zmax[i], fmaxf(fmaxf(z[h][i][0], z[h][i][1]), fmaxf(z[h][i][2], z[h][i][3])));
+      smax = fmaxf(smax, fmaxf(fmaxf(step[h][0], step[h][1]), fmaxf(step[h][2], step[h][3])));
     }
-    const float zmax = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]));
-    const float smax = fmaxf(fmaxf(step[0], step[1]), fmaxf(step[2], step[3]));
-    if (__any_sync(0xffffffffu, zmax > m + SLACK || smax > top)) {
+    bool raise = smax > top;
+#pragma unroll
+    for (int i = 0; i < NR; ++i) raise = raise || zmax[i] > m[i] + SLACK;
+    if (__any_sync(0xffffffffu, raise)) {
       float wide = smax;
 #pragma unroll
       for (int s = 16; s; s >>= 1) wide = fmaxf(wide, __shfl_xor_sync(0xffffffffu, wide, s));
@@ -250,133 +345,228 @@ __global__ void __launch_bounds__(WARPS * 32) attn_kv4_kernel(const __grid_const
         inv_top = __uint_as_float((254 - e) << 23);
         shrink = was * inv_top;
       }
-      const float raised = fmaxf(m, quad_max(zmax) - BELOW);
-      const float a = exp2f(m - raised);
-      m = raised;
-      l *= a;
-      bs *= a;
+      float a[NR];
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        const float raised = fmaxf(m[i], quad_max(zmax[i]) - BELOW);
+        a[i] = exp2f(m[i] - raised);
+        m[i] = raised;
+        l[i] *= a[i];
+        bs[i] *= a[i];
+        a[i] *= shrink;
+      }
 #pragma unroll
       for (int j = 0; j < HD / 8; ++j) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[j][i] *= a * shrink;
+        for (int i = 0; i < 4; ++i) o[j][i] *= a[PRECISE ? 0 : i / 2];
       }
     }
-    float w[4];
+    uint32_t wf[2][4];  // the weights as A fragments
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float e = exp2f(z[i] - m);
-      l += e;
-      bs = fmaf(e, base[i], bs);
-      w[i] = e * (step[i] * inv_top);
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        float w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float e = pow2(z[h][i][j] - m[i]);
+          l[i] += e;
+          bs[i] = fmaf(e, base[h][j], bs[i]);
+          w[j] = e * (step[h][j] * inv_top);
+        }
+        if (PRECISE) {
+          split_f16(w[0], w[1], wf[h][0], wf[h][1]);
+          split_f16(w[2], w[3], wf[h][2], wf[h][3]);
+        } else {
+          wf[h][i] = pack_f16(w[0], w[1]);
+          wf[h][2 + i] = pack_f16(w[2], w[3]);
+        }
+      }
     }
-    uint32_t h0, l0, h1, l1;
-    split_f16(w[0], w[1], h0, l0);
-    split_f16(w[2], w[3], h1, l1);
     // V: row pairs t and t + 4, channels [CHUNK r, CHUNK (r + 1))
     constexpr int NV = HD / 32;
-    uint32_t va[NV], vb[NV];
-    const unsigned char* v0 = page + P::V + t * 2 * P::ROW + P::place(t, r) * P::CHUNK;
-    const unsigned char* v1 = page + P::V + (t + 4) * 2 * P::ROW + P::place(t + 4, r) * P::CHUNK;
-    if (NV == 4) {
-      *reinterpret_cast<uint4*>(va) = *reinterpret_cast<const uint4*>(v0);
-      *reinterpret_cast<uint4*>(vb) = *reinterpret_cast<const uint4*>(v1);
-    } else {
-      *reinterpret_cast<uint2*>(va) = *reinterpret_cast<const uint2*>(v0);
-      *reinterpret_cast<uint2*>(vb) = *reinterpret_cast<const uint2*>(v1);
+    uint32_t v[2][2][NV];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const unsigned char* at = page[h] + P::V + (t + 4 * i) * 2 * P::ROW + P::place(t + 4 * i, r) * P::CHUNK;
+        if (NV == 4)
+          *reinterpret_cast<uint4*>(v[h][i]) = *reinterpret_cast<const uint4*>(at);
+        else
+          *reinterpret_cast<uint2*>(v[h][i]) = *reinterpret_cast<const uint2*>(at);
+      }
     }
 #pragma unroll
     for (int c = 0; c < NV; ++c) {
       uint32_t u[4], x[4];
-      kv4_codes(va[c], u);
-      kv4_codes(vb[c], x);
+      float d[4][4];
+      kv4_codes(v[0][0][c], u);
+      kv4_codes(v[0][1][c], x);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) mma_f16(o[4 * c + i], h0, l0, h1, l1, u[i], x[i]);
+      for (int i = 0; i < 4; ++i) {
+        // the tensor cores round their sums toward zero: in a chain over all pages that is a bias
+        if (PRECISE)
+          mma_f16_first(d[i], wf[0][0], wf[0][1], wf[0][2], wf[0][3], u[i], x[i]);
+        else
+          mma_f16(o[4 * c + i], wf[0][0], wf[0][1], wf[0][2], wf[0][3], u[i], x[i]);
+      }
+      kv4_codes(v[1][0][c], u);
+      kv4_codes(v[1][1][c], x);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (PRECISE) {
+          mma_f16(d[i], wf[1][0], wf[1][1], wf[1][2], wf[1][3], u[i], x[i]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[4 * c + i][j] += d[i][j];
+        } else {
+          mma_f16(o[4 * c + i], wf[1][0], wf[1][1], wf[1][2], wf[1][3], u[i], x[i]);
+        }
+      }
     }
     __syncwarp();
-    if (lane == 0 && k + STAGES < mine) request(k + STAGES);
+    if (RTW > 1 && lane == 0) {
+      mbar_arrive(empty + stage);
+      mbar_arrive(empty + stage + 1);
+    }
+    stage += 2;
+    if (stage == STAGES) {
+      stage = 0;
+      phase ^= 1;
+    }
+    // the two pages after the next pair, into the places of the pair before this one
+    if (lane == 0 && rt == 0 && asked < mine) {
+      for (int i = 0; i < 2 && asked < mine; ++i) {
+        const int at = asked % STAGES;
+        if (RTW > 1 && asked >= STAGES && !mbar_wait(empty + at, (asked / STAGES - 1) & 1, &sh_abort, WAIT_NS)) break;
+        request();
+      }
+    }
+    __syncwarp();
   }
 
-  // rows of the warp: column c of sums [r][HD], over the ring (all of its pages have been read)
-  l = quad_sum(l);
-  bs = quad_sum(bs);
-  float* sums = reinterpret_cast<float*>(ring);
+  // the block's sums, over the rings: column c of [warp][row][HD]
+#pragma unroll
+  for (int i = 0; i < NR; ++i) {
+    l[i] = quad_sum(l[i]);
+    bs[i] = quad_sum(bs[i]);
+  }
+  if (lane == 0 && rt == 0 && sh_abort)  // copies still in flight land before the rings are used again
+    for (int i = max(0, asked - STAGES); i < asked; ++i) mbar_wait_plain(full + i % STAGES, i / STAGES & 1, WAIT_NS);
   float* ml = reinterpret_cast<float*>(smem + S::ML);
-  __syncwarp();
+  __syncthreads();
+  float* sums = reinterpret_cast<float*>(smem) + warp * TILE * HD;
 #pragma unroll
   for (int j = 0; j < HD / 8; ++j) {
-    sums[r * HD + 2 * t * P::CHUNK + j] = fmaf(o[j][0] + o[j][2], top, bs);
-    sums[r * HD + (2 * t + 1) * P::CHUNK + j] = fmaf(o[j][1] + o[j][3], top, bs);
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      sums[(r + 8 * i) * HD + 2 * t * P::CHUNK + j] = fmaf(PRECISE ? o[j][0] + o[j][2] : o[j][2 * i], top, bs[i]);
+      sums[(r + 8 * i) * HD + (2 * t + 1) * P::CHUNK + j] = fmaf(PRECISE ? o[j][1] + o[j][3] : o[j][2 * i + 1], top, bs[i]);
+    }
   }
-  if (t == 0) {
-    ml[(warp * ROWS + r) * 2] = m;
-    ml[(warp * ROWS + r) * 2 + 1] = l;
-  }
+#pragma unroll
+  for (int i = 0; i < NR; ++i)
+    if (t == 0) {
+      ml[(warp * TILE + r + 8 * i) * 2] = m[i];
+      ml[(warp * TILE + r + 8 * i) * 2 + 1] = l[i];
+    }
   __syncthreads();
 
-  // the block's rows: warp r merges row r over the warps
-  const int my = warp;
-  const int mrow = tile * ROWS + my;
-  float M = NONE, L = 0.f, f[WARPS];
+  constexpr int LINE = HD + 4;
+  float* ws = p.ws + static_cast<size_t>(blockIdx.y) * splits * S::ROWS * LINE;
+  const int here = min(S::ROWS, n_rows - row0);
+  for (int my = warp; my < here; my += WARPS) {  // a warp merges a row over the slices
+    const int w0 = my / TILE, at = my % TILE;
+    float M = NONE, L = 0.f, f[S::SLICES], acc[HD / 32] = {};
 #pragma unroll
-  for (int w = 0; w < WARPS; ++w) M = fmaxf(M, ml[(w * ROWS + my) * 2]);
+    for (int w = 0; w < S::SLICES; ++w) M = fmaxf(M, ml[((w0 + w * RTW) * TILE + at) * 2]);
 #pragma unroll
-  for (int w = 0; w < WARPS; ++w) {
-    f[w] = exp2f(ml[(w * ROWS + my) * 2] - M);
-    L = fmaf(f[w], ml[(w * ROWS + my) * 2 + 1], L);
-  }
-  float acc[HD / 32];
+    for (int w = 0; w < S::SLICES; ++w) {
+      f[w] = exp2f(ml[((w0 + w * RTW) * TILE + at) * 2] - M);
+      L = fmaf(f[w], ml[((w0 + w * RTW) * TILE + at) * 2 + 1], L);
 #pragma unroll
-  for (int i = 0; i < HD / 32; ++i) {
-    acc[i] = 0.f;
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w)
-      acc[i] = fmaf(f[w], reinterpret_cast<const float*>(smem + w * S::RING)[my * HD + lane + 32 * i], acc[i]);
-  }
-  if (splits > 1) {
-    constexpr int LINE = HD + 2;
-    float* ws = p.ws + (static_cast<size_t>(blockIdx.y) * splits * ROWS) * LINE;
-    float* line = ws + (split * ROWS + my) * LINE;
+      for (int i = 0; i < HD / 32; ++i)
+        acc[i] = fmaf(f[w], reinterpret_cast<const float*>(smem)[((w0 + w * RTW) * TILE + at) * HD + lane + 32 * i], acc[i]);
+    }
+    if (splits == 1) {
+      store_row<HD>(p, bg, row0 + my, lane, M, L, acc);
+      continue;
+    }
+    float* line = ws + (split * S::ROWS + my) * LINE;
 #pragma unroll
     for (int i = 0; i < HD / 32; ++i) line[lane + 32 * i] = acc[i];
     if (lane == 0) {
       line[HD] = M;
       line[HD + 1] = L;
     }
-    __threadfence();
-    __syncthreads();
-    if (tid == 0) {
-      const int seen_before = atomicAdd(p.counters + blockIdx.y, 1);
-      sh_last = seen_before == splits - 1;
-      if (sh_last) p.counters[blockIdx.y] = 0;
+  }
+}
+
+// Merges the splits of a row: four warps take every fourth split, and their sums are added in the warps' order.  (By the
+// last block of the tile to arrive, 64 rows of 15 splits took longer than the attention itself.)
+template <int HD>
+__global__ void __launch_bounds__(128) join_kv4_kernel(const __grid_constant__ Kv4AttnParams p, int rows, int blocks) {
+  constexpr int LINE = HD + 4, W = HD / 32;  // W: columns of a lane
+  __shared__ float sh_acc[4][HD];
+  pdl_wait();
+  pdl_trigger();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, n_rows = p.nq * (p.H / p.c.G);
+  const int bg = static_cast<int>(blockIdx.x / n_rows), row = static_cast<int>(blockIdx.x % n_rows), splits = p.splits;
+  const float* ws = p.ws + (static_cast<size_t>(bg * blocks + row / rows) * splits * rows + row % rows) * LINE;
+  const size_t step = static_cast<size_t>(rows) * LINE;
+  // reference and sum of split lane, and of split 32 + lane
+  float m[2], l[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const bool there = lane + 32 * i < splits;
+    m[i] = there ? ws[(lane + 32 * i) * step + HD] : NONE;
+    l[i] = there ? ws[(lane + 32 * i) * step + HD + 1] : 0.f;
+  }
+  float acc[W] = {};
+  constexpr int ONCE = 4;
+  float v[ONCE][W];
+  auto fetch = [&](int s0) {
+#pragma unroll
+    for (int i = 0; i < ONCE; ++i) {
+      const float* part = ws + min(s0 + 4 * i, splits - 1) * step + W * lane;
+      if constexpr (W == 4)
+        *reinterpret_cast<float4*>(v[i]) = *reinterpret_cast<const float4*>(part);
+      else
+        *reinterpret_cast<float2*>(v[i]) = *reinterpret_cast<const float2*>(part);
     }
-    __syncthreads();
-    if (!sh_last) return;
-    __threadfence();
-    M = NONE;
-    for (int s = 0; s < splits; ++s) M = fmaxf(M, __ldcg(ws + (s * ROWS + my) * LINE + HD));
-    L = 0.f;
+  };
+  fetch(warp);
+  float M = fmaxf(m[0], m[1]);
 #pragma unroll
-    for (int i = 0; i < HD / 32; ++i) acc[i] = 0.f;
-    for (int s = 0; s < splits; ++s) {
-      const float* part = ws + (s * ROWS + my) * LINE;
-      const float e = exp2f(__ldcg(part + HD) - M);
-      L = fmaf(e, __ldcg(part + HD + 1), L);
+  for (int s = 16; s; s >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, s));
+  const float f[2] = {exp2f(m[0] - M), exp2f(m[1] - M)};
+  float L = fmaf(f[0], l[0], f[1] * l[1]);
 #pragma unroll
-      for (int i = 0; i < HD / 32; ++i) acc[i] = fmaf(e, __ldcg(part + lane + 32 * i), acc[i]);
+  for (int s = 16; s; s >>= 1) L += __shfl_xor_sync(0xffffffffu, L, s);
+  for (int s0 = warp; s0 < splits; s0 += 4 * ONCE) {
+    if (s0 != warp) fetch(s0);
+#pragma unroll
+    for (int i = 0; i < ONCE; ++i) {
+      const int s = s0 + 4 * i;
+      const float e = __shfl_sync(0xffffffffu, s & 32 ? f[1] : f[0], s & 31);
+      if (s >= splits) break;
+#pragma unroll
+      for (int j = 0; j < W; ++j) acc[j] = fmaf(e, v[i][j], acc[j]);
     }
   }
-  if (mrow >= n_rows) return;
-  const int oi = mrow / group, oh = g * group + mrow % group;
-  const size_t orow = static_cast<size_t>(b) * p.q_rows + oi;
-  const float inv = L == 0.f ? 0.f : 1.f / L;  // a row that sees nothing gives zeros
 #pragma unroll
-  for (int i = 0; i < HD / 32; ++i) store_out(p, orow * p.ldo + oh * HD + lane + 32 * i, acc[i] * inv);
-  if (p.lse && lane == 0) p.lse[orow * p.H + oh] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+  for (int j = 0; j < W; ++j) sh_acc[warp][W * lane + j] = acc[j];
+  __syncthreads();
+  if (warp) return;
+#pragma unroll
+  for (int j = 0; j < W; ++j) acc[j] = (sh_acc[0][lane + 32 * j] + sh_acc[1][lane + 32 * j]) + (sh_acc[2][lane + 32 * j] + sh_acc[3][lane + 32 * j]);
+  store_row<HD>(p, bg, row, lane, M, L, acc);
 }
 
 // ---------------------------------------------------------------------------
 // attention weight per cached row
 // ---------------------------------------------------------------------------
+constexpr int STAGES = 4, ROWS = 8;
 constexpr int SCORE_TILES = 8;  // row tiles whose fragments are held in shared memory at a time
 
 template <int HD>
@@ -473,7 +663,7 @@ __global__ void __launch_bounds__(WARPS * 32) score_kv4_kernel(const __grid_cons
 #pragma unroll
         for (int j = 0; j < HD / 16; ++j)
           *reinterpret_cast<uint4*>(f[j]) = reinterpret_cast<const uint4*>(smem + S::FRAGS)[(i * (HD / 16) + j) * 32 + lane];
-        float s0[4] = {}, s1[4] = {};
+        float s0[4], s1[4];
         page_dots<HD>(page, f, r, t, s0, s1);
         const float4 rf = reinterpret_cast<const float4*>(smem + S::ROWF)[i * ROWS + r];
         Seen seen = all;
@@ -482,7 +672,7 @@ __global__ void __launch_bounds__(WARPS * 32) score_kv4_kernel(const __grid_cons
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           const float z = fmaf(step[x] * rf.x, d[x], base[x] * rf.y);
-          if (rf.w != 0.f && (whole || seen(slot0 + 2 * t + (x & 1) + 8 * (x >> 1)))) sum[x] = fmaf(rf.w, exp2f(z - rf.z), sum[x]);
+          if (rf.w != 0.f && (whole || seen(slot0 + 2 * t + (x & 1) + 8 * (x >> 1)))) sum[x] = fmaf(rf.w, pow2(z - rf.z), sum[x]);
         }
       }
 #pragma unroll
@@ -507,26 +697,61 @@ cudaError_t launch_sized(K kernel, size_t smem, dim3 grid, const Kv4AttnParams& 
 
 }  // namespace
 
-int kv4_attn_row_tiles(int nq, int H, int G) { return (nq * (H / G) + ROWS - 1) / ROWS; }
+// How a call's rows are cut: one term per query where the result is rounded to bf16 alone and there are rows
+// enough to fill its tiles, and warps that share pages when there are several tiles.
+namespace {
+struct Cut {
+  bool precise;
+  int rtw, rows;  // tiles at a time, rows of a block
+};
+Cut cut_of(const Kv4AttnParams& p) {
+  const int rows = p.nq * (p.H / p.c.G);
+  const bool precise = rows <= 8 || p.out_f32 || p.out_lo || p.lse;
+  const int tile = precise ? 8 : 16, tiles = (rows + tile - 1) / tile;
+  const int rtw = tiles == 1 ? 1 : tiles == 2 ? 2 : 4;
+  return Cut{precise, rtw, tile * rtw};
+}
+int blocks_of(const Kv4AttnParams& p) {
+  const Cut c = cut_of(p);
+  return (p.nq * (p.H / p.c.G) + c.rows - 1) / c.rows * p.c.B * p.c.G;
+}
+}  // namespace
+
+int kv4_attn_blocks(const Kv4AttnParams& p) { return blocks_of(p); }
 
 int kv4_attn_splits(const Kv4AttnParams& p) {
-  const int tiles = kv4_attn_row_tiles(p.nq, p.H, p.c.G) * p.c.B * p.c.G;
-  const int want = (2 * tc_num_sms() + tiles - 1) / tiles;
-  const int most = (p.c.max_pages + WARPS - 1) / WARPS;
-  return want < 1 ? 1 : want > most ? most : want > 64 ? 64 : want;
+  const Cut c = cut_of(p);
+  const int blocks = blocks_of(p), pairs = (p.c.max_pages + 2 * WARPS / c.rtw - 1) / (2 * WARPS / c.rtw);
+  const int want = 3 * tc_num_sms() / blocks;  // three blocks per SM, and none left for a second wave
+  return std::max(1, std::min(std::min(want, pairs), 64));
 }
 
 size_t kv4_attn_ws_floats(const Kv4AttnParams& p) {
-  return static_cast<size_t>(kv4_attn_row_tiles(p.nq, p.H, p.c.G)) * p.c.B * p.c.G * p.splits * ROWS * (p.c.hd + 2);
+  return static_cast<size_t>(blocks_of(p)) * p.splits * cut_of(p).rows * (p.c.hd + 4);
 }
 
+namespace {
+template <int HD, typename TQ, bool PRECISE, int RTW>
+cudaError_t launch_attn(const Kv4AttnParams& p, cudaStream_t s) {
+  const int blocks = blocks_of(p);
+  const cudaError_t e = launch_sized(attn_kv4_kernel<HD, TQ, PRECISE, RTW>, Shape<HD, PRECISE, RTW>::BYTES, dim3(p.splits, blocks), p, s);
+  if (e != cudaSuccess || p.splits == 1) return e;
+  const long long rows = static_cast<long long>(p.nq) * p.c.B * p.H;
+  return launch_pdl(join_kv4_kernel<HD>, dim3(static_cast<unsigned>(rows)), dim3(128), 0, s, p, Shape<HD, PRECISE, RTW>::ROWS,
+                    blocks / (p.c.B * p.c.G));
+}
+template <int HD, typename TQ>
+cudaError_t launch_cut(const Kv4AttnParams& p, cudaStream_t s) {
+  const Cut c = cut_of(p);
+  if (c.precise)
+    return c.rtw == 1 ? launch_attn<HD, TQ, true, 1>(p, s) : c.rtw == 2 ? launch_attn<HD, TQ, true, 2>(p, s) : launch_attn<HD, TQ, true, 4>(p, s);
+  return c.rtw == 1 ? launch_attn<HD, TQ, false, 1>(p, s) : c.rtw == 2 ? launch_attn<HD, TQ, false, 2>(p, s) : launch_attn<HD, TQ, false, 4>(p, s);
+}
+}  // namespace
+
 cudaError_t attention_kv4(const Kv4AttnParams& p, cudaStream_t s) {
-  const dim3 grid(p.splits, kv4_attn_row_tiles(p.nq, p.H, p.c.G) * p.c.B * p.c.G);
-  if (p.c.hd == 128)
-    return p.q_f32 ? launch_sized(attn_kv4_kernel<128, float>, Smem<128>::BYTES, grid, p, s)
-                   : launch_sized(attn_kv4_kernel<128, bf16>, Smem<128>::BYTES, grid, p, s);
-  return p.q_f32 ? launch_sized(attn_kv4_kernel<64, float>, Smem<64>::BYTES, grid, p, s)
-                 : launch_sized(attn_kv4_kernel<64, bf16>, Smem<64>::BYTES, grid, p, s);
+  if (p.c.hd == 128) return p.q_f32 ? launch_cut<128, float>(p, s) : launch_cut<128, bf16>(p, s);
+  return p.q_f32 ? launch_cut<64, float>(p, s) : launch_cut<64, bf16>(p, s);
 }
 
 cudaError_t kv4_score(const Kv4AttnParams& p, cudaStream_t s) {

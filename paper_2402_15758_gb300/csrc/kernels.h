@@ -386,13 +386,12 @@ struct Kv4AttnParams {
   float* lse;         // optional [B * q_rows][H]; the score kernel's input
   int splits;
   float* ws;
-  int* counters;      // [B * G * row tiles], zero between launches
   // score: scores[(b * G + g) * ld_scores + slot] += sum over the rows of weight p
   float* scores;
   int ld_scores;
   const float* weight;  // optional [B * q_rows]
 };
-int kv4_attn_row_tiles(int nq, int H, int G);
+int kv4_attn_blocks(const Kv4AttnParams& p);  // of the grid, without its splits
 int kv4_attn_splits(const Kv4AttnParams& p);
 size_t kv4_attn_ws_floats(const Kv4AttnParams& p);
 cudaError_t attention_kv4(const Kv4AttnParams& p, cudaStream_t s);

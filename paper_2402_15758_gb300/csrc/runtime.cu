@@ -2234,8 +2234,7 @@ chimera_status chimera_op_attention_kv4(int q_dtype, int out_dtype, int batch, i
   p.ldo = ldo;
   p.lse = lse;
   p.splits = splits ? splits : kv4_attn_splits(p);
-  const long long tiles = static_cast<long long>(kv4_attn_row_tiles(nq, n_heads, kv_heads)) * batch * kv_heads;
-  if (tiles > OP_ATT_COUNTERS) return CHIMERA_EINVAL;
+  if (kv4_attn_blocks(p) > 65535) return CHIMERA_EINVAL;
   while (p.splits > 1 && kv4_attn_ws_floats(p) > OP_ATT_FLOATS) --p.splits;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   std::lock_guard<std::mutex> lk(g_op_mu);
@@ -2243,7 +2242,6 @@ chimera_status chimera_op_attention_kv4(int q_dtype, int out_dtype, int batch, i
   if (!sc) return CHIMERA_ENOMEM;
   p.c.err = sc->err;
   p.ws = sc->att_ws;
-  p.counters = sc->att_cnt;
   const cudaError_t e = attention_kv4(p, s);
   return op_done(sc, s) && e == cudaSuccess ? CHIMERA_OK : CHIMERA_ECUDA;
 }
