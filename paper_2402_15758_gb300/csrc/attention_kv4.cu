@@ -190,14 +190,17 @@ __device__ __forceinline__ void store_out(const Kv4AttnParams& p, size_t at, T v
   store_act(static_cast<bf16*>(p.out), reinterpret_cast<bf16*>(p.out_lo), at, v);
 }
 
-// Writes a merged row (of the rows of a sequence and kv head): lane l has columns l, l + 32, ..
+// Writes a merged row (of the rows of a sequence and kv head) from its sums in shared memory.
 template <int HD>
-__device__ __forceinline__ void store_row(const Kv4AttnParams& p, int bg, int row, int lane, float M, float L, const float (&acc)[HD / 32]) {
+__device__ __forceinline__ void store_row(const Kv4AttnParams& p, int bg, int row, int lane, float M, float L, const float* sums) {
   const int group = p.H / p.c.G, head = bg % p.c.G * group + row % group;
   const size_t out = static_cast<size_t>(bg / p.c.G) * p.q_rows + row / group;
   const float inv = L == 0.f ? 0.f : 1.f / L;  // a row that sees nothing gives zeros
 #pragma unroll
-  for (int i = 0; i < HD / 32; ++i) store_out(p, out * p.ldo + head * HD + lane + 32 * i, acc[i] * inv);
+  for (int i = 0; i < HD / 32; ++i) {
+    const int c = lane + 32 * i;
+    store_out(p, out * p.ldo + head * HD + c, sums[c % Kv4<HD>::CHUNK * 8 + c / Kv4<HD>::CHUNK] * inv);
+  }
   if (p.lse && lane == 0) p.lse[out * p.H + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
 }
 
@@ -206,9 +209,10 @@ __device__ __forceinline__ void store_row(const Kv4AttnParams& p, int bg, int ro
 template <int HD, bool PRECISE, int RTW>
 struct Shape {
   static constexpr int TILE = PRECISE ? 8 : 16, ROWS = TILE * RTW, SLICES = WARPS / RTW;
-  static constexpr int STAGES = 6;  // pages of a slice: three pairs
+  static constexpr int STAGES = 8;  // pages of a slice: four pairs
   static constexpr int RING = STAGES * Kv4<HD>::BYTES;
-  static constexpr int SUMS = WARPS * TILE * HD * 4;  // over the rings
+  static constexpr int PITCH = HD + 8;  // of a row of sums: in the order of the products' columns
+  static constexpr int SUMS = WARPS * TILE * PITCH * 4;  // over the rings
   static constexpr int BARS = SLICES * RING > SUMS ? SLICES * RING : SUMS;
   static constexpr int ML = BARS + SLICES * STAGES * 16;  // reference and sum of each warp's rows
   static constexpr int BYTES = ML + WARPS * TILE * 8;
@@ -288,30 +292,45 @@ __global__ void __launch_bounds__(WARPS * 32, 3) attn_kv4_kernel(const __grid_co
 #pragma unroll
   for (int i = 0; i < NR; ++i) m[i] = NONE, l[i] = bs[i] = 0.f;
   float top = 0x1p-126f, inv_top = 0x1p126f;  // power of two above every V step so far
-  int stage = 0;
+  // The products of a pair with the queries are taken one pair ahead, so that they overlap the softmax before.
+  int stage = 0;  // of the pair whose products come next
   uint32_t phase = 0;
-  for (int k = 0; k < mine; k += 2) {
+  float dots[2][2][4], ahead[2][2][4];  // [page][keys 0..7, 8..15]
+  bool ok = true;
+  auto products = [&](int k, float (&d)[2][2][4]) {
     const bool two = k + 1 < mine;
-    if (!mbar_wait_warp(full + stage, phase, &sh_abort, WAIT_NS) || (two && !mbar_wait_warp(full + stage + 1, phase, &sh_abort, WAIT_NS))) {
-      if (lane == 0) atomicOr(p.c.err, ERR_TIMEOUT);
-      break;
+    ok = mbar_wait_warp(full + stage, phase, &sh_abort, WAIT_NS) && (!two || mbar_wait_warp(full + stage + 1, phase, &sh_abort, WAIT_NS));
+    if (!ok) return;
+    page_dots<HD>(ring + stage * P::BYTES, qf, r, t, d[0][0], d[0][1]);
+    page_dots<HD>(ring + (stage + (two ? 1 : 0)) * P::BYTES, qf, r, t, d[1][0], d[1][1]);
+    stage += 2;
+    if (stage == STAGES) {
+      stage = 0;
+      phase ^= 1;
     }
-    const unsigned char* page[2] = {ring + stage * P::BYTES, ring + (stage + (two ? 1 : 0)) * P::BYTES};
+  };
+  if (mine > 0) products(0, dots);
+  for (int k = 0; ok && k < mine; k += 2) {
+    const bool two = k + 1 < mine;
+    const int now = k % STAGES;  // stage of this pair
+    if (k + 2 < mine) products(k + 2, ahead);
+    if (!ok) break;
+    const unsigned char* page[2] = {ring + now * P::BYTES, ring + (now + (two ? 1 : 0)) * P::BYTES};
     float z[2][NR][4], step[2][4], base[2][4];
     float zmax[NR], smax = 0.f;
 #pragma unroll
     for (int i = 0; i < NR; ++i) zmax[i] = -INFINITY;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      float s0[4], s1[4];
-      page_dots<HD>(page[h], qf, r, t, s0, s1);
       key_scales(page[h] + P::KS, t, step[h], base[h]);
 #pragma unroll
       for (int i = 0; i < NR; ++i) {
-        const float d[4] = {PRECISE ? s0[0] + s0[2] : s0[2 * i], PRECISE ? s0[1] + s0[3] : s0[2 * i + 1],
-                            PRECISE ? s1[0] + s1[2] : s1[2 * i], PRECISE ? s1[1] + s1[3] : s1[2 * i + 1]};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) z[h][i][j] = fmaf(step[h][j] * q_scale[i], d[j], base[h][j] * q_sum[i]);
+        for (int j = 0; j < 4; ++j) {
+          const float* s = dots[h][j / 2];
+          const float d = PRECISE ? s[j % 2] + s[2 + j % 2] : s[2 * i + j % 2];
+          z[h][i][j] = fmaf(step[h][j] * q_scale[i], d, base[h][j] * q_sum[i]);
+        }
       }
       key_scales(page[h] + P::VS, t, step[h], base[h]);
       const int slot0 = (p0 + slice + (k + h) * S::SLICES) * KV4_ROWS;
@@ -424,17 +443,17 @@ __global__ void __launch_bounds__(WARPS * 32, 3) attn_kv4_kernel(const __grid_co
         }
       }
     }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) dots[h][i / 4][i % 4] = ahead[h][i / 4][i % 4];
+    }
     __syncwarp();
     if (RTW > 1 && lane == 0) {
-      mbar_arrive(empty + stage);
-      mbar_arrive(empty + stage + 1);
+      mbar_arrive(empty + now);
+      mbar_arrive(empty + now + 1);
     }
-    stage += 2;
-    if (stage == STAGES) {
-      stage = 0;
-      phase ^= 1;
-    }
-    // the two pages after the next pair, into the places of the pair before this one
+    // the pair after the next two, into the places of the pair before this one
     if (lane == 0 && rt == 0 && asked < mine) {
       for (int i = 0; i < 2 && asked < mine; ++i) {
         const int at = asked % STAGES;
@@ -444,8 +463,9 @@ __global__ void __launch_bounds__(WARPS * 32, 3) attn_kv4_kernel(const __grid_co
     }
     __syncwarp();
   }
+  if (!ok && lane == 0) atomicOr(p.c.err, ERR_TIMEOUT);
 
-  // the block's sums, over the rings: column c of [warp][row][HD]
+  // the block's sums, over the rings: channel CHUNK n + j of a row at 8 j + n
 #pragma unroll
   for (int i = 0; i < NR; ++i) {
     l[i] = quad_sum(l[i]);
@@ -455,14 +475,14 @@ __global__ void __launch_bounds__(WARPS * 32, 3) attn_kv4_kernel(const __grid_co
     for (int i = max(0, asked - STAGES); i < asked; ++i) mbar_wait_plain(full + i % STAGES, i / STAGES & 1, WAIT_NS);
   float* ml = reinterpret_cast<float*>(smem + S::ML);
   __syncthreads();
-  float* sums = reinterpret_cast<float*>(smem) + warp * TILE * HD;
+  float* sums = reinterpret_cast<float*>(smem) + warp * TILE * S::PITCH;
 #pragma unroll
   for (int j = 0; j < HD / 8; ++j) {
 #pragma unroll
-    for (int i = 0; i < NR; ++i) {
-      sums[(r + 8 * i) * HD + 2 * t * P::CHUNK + j] = fmaf(PRECISE ? o[j][0] + o[j][2] : o[j][2 * i], top, bs[i]);
-      sums[(r + 8 * i) * HD + (2 * t + 1) * P::CHUNK + j] = fmaf(PRECISE ? o[j][1] + o[j][3] : o[j][2 * i + 1], top, bs[i]);
-    }
+    for (int i = 0; i < NR; ++i)
+      *reinterpret_cast<float2*>(sums + (r + 8 * i) * S::PITCH + 8 * j + 2 * t) =
+          make_float2(fmaf(PRECISE ? o[j][0] + o[j][2] : o[j][2 * i], top, bs[i]),
+                      fmaf(PRECISE ? o[j][1] + o[j][3] : o[j][2 * i + 1], top, bs[i]));
   }
 #pragma unroll
   for (int i = 0; i < NR; ++i)
@@ -477,7 +497,9 @@ __global__ void __launch_bounds__(WARPS * 32, 3) attn_kv4_kernel(const __grid_co
   const int here = min(S::ROWS, n_rows - row0);
   for (int my = warp; my < here; my += WARPS) {  // a warp merges a row over the slices
     const int w0 = my / TILE, at = my % TILE;
-    float M = NONE, L = 0.f, f[S::SLICES], acc[HD / 32] = {};
+    constexpr int W = HD / 32;
+    float M = NONE, L = 0.f, f[S::SLICES], acc[W] = {};
+    float* mine = reinterpret_cast<float*>(smem) + (w0 * TILE + at) * S::PITCH + W * lane;
 #pragma unroll
     for (int w = 0; w < S::SLICES; ++w) M = fmaxf(M, ml[((w0 + w * RTW) * TILE + at) * 2]);
 #pragma unroll
@@ -485,16 +507,20 @@ __global__ void __launch_bounds__(WARPS * 32, 3) attn_kv4_kernel(const __grid_co
       f[w] = exp2f(ml[((w0 + w * RTW) * TILE + at) * 2] - M);
       L = fmaf(f[w], ml[((w0 + w * RTW) * TILE + at) * 2 + 1], L);
 #pragma unroll
-      for (int i = 0; i < HD / 32; ++i)
-        acc[i] = fmaf(f[w], reinterpret_cast<const float*>(smem)[((w0 + w * RTW) * TILE + at) * HD + lane + 32 * i], acc[i]);
+      for (int i = 0; i < W; ++i) acc[i] = fmaf(f[w], mine[w * RTW * TILE * S::PITCH + i], acc[i]);
     }
     if (splits == 1) {
-      store_row<HD>(p, bg, row0 + my, lane, M, L, acc);
+#pragma unroll
+      for (int i = 0; i < W; ++i) mine[i] = acc[i];
+      __syncwarp();
+      store_row<HD>(p, bg, row0 + my, lane, M, L, mine - W * lane);
       continue;
     }
     float* line = ws + (split * S::ROWS + my) * LINE;
-#pragma unroll
-    for (int i = 0; i < HD / 32; ++i) line[lane + 32 * i] = acc[i];
+    if constexpr (W == 4)
+      *reinterpret_cast<float4*>(line + W * lane) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    else
+      *reinterpret_cast<float2*>(line + W * lane) = make_float2(acc[0], acc[1]);
     if (lane == 0) {
       line[HD] = M;
       line[HD + 1] = L;
@@ -559,8 +585,10 @@ __global__ void __launch_bounds__(128) join_kv4_kernel(const __grid_constant__ K
   __syncthreads();
   if (warp) return;
 #pragma unroll
-  for (int j = 0; j < W; ++j) acc[j] = (sh_acc[0][lane + 32 * j] + sh_acc[1][lane + 32 * j]) + (sh_acc[2][lane + 32 * j] + sh_acc[3][lane + 32 * j]);
-  store_row<HD>(p, bg, row, lane, M, L, acc);
+  for (int j = 0; j < W; ++j)
+    sh_acc[0][lane + 32 * j] = (sh_acc[0][lane + 32 * j] + sh_acc[1][lane + 32 * j]) + (sh_acc[2][lane + 32 * j] + sh_acc[3][lane + 32 * j]);
+  __syncwarp();
+  store_row<HD>(p, bg, row, lane, M, L, sh_acc[0]);
 }
 
 // ---------------------------------------------------------------------------
