@@ -613,7 +613,7 @@ __global__ void __launch_bounds__(WARPS * 32) score_kv4_kernel(const __grid_cons
   extern __shared__ __align__(128) unsigned char smem[];
   using S = ScoreSmem<HD>;
   using P = Kv4<HD>;
-  __shared__ int sh_abort;
+  __shared__ int sh_abort, sh_queries, sh_query[64];
   const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31, r = lane / 4, t = lane & 3;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::BARS) + warp * STAGES;
   unsigned char* ring = smem + warp * S::RING;
@@ -626,8 +626,20 @@ __global__ void __launch_bounds__(WARPS * 32) score_kv4_kernel(const __grid_cons
   pdl_wait();
   pdl_trigger();
 
-  const int group = p.H / p.c.G, n_rows = p.nq * group, tiles = (n_rows + ROWS - 1) / ROWS;
-  const int bg = blockIdx.y, b = bg / p.c.G, g = bg % p.c.G;
+  const int group = p.H / p.c.G, bg = blockIdx.y, b = bg / p.c.G, g = bg % p.c.G;
+  // the queries that count
+  if (warp == 0) {
+    int found = 0;
+    for (int i = lane; i < (p.nq + 31) / 32 * 32; i += 32) {
+      const bool counts = i < p.nq && (!p.weight || p.weight[static_cast<size_t>(b) * p.q_rows + i] != 0.f);
+      const uint32_t all = __ballot_sync(0xffffffffu, counts);
+      if (counts) sh_query[found + __popc(all & ((1u << lane) - 1))] = i;
+      found += __popc(all);
+    }
+    if (lane == 0) sh_queries = found;
+  }
+  __syncthreads();
+  const int n_rows = sh_queries * group, tiles = (n_rows + ROWS - 1) / ROWS;
   const Seen all = what_is_seen(p, b);
   const int pages = (min(all.total, p.ld_scores) + KV4_ROWS - 1) / KV4_ROWS;
   if (all.total > p.ld_scores && tid == 0) atomicOr(p.c.err, ERR_CAPACITY);
@@ -656,7 +668,7 @@ __global__ void __launch_bounds__(WARPS * 32) score_kv4_kernel(const __grid_cons
     for (int i = warp; i < held; i += WARPS) {
       const int row = (tile0 + i) * ROWS + r;
       const bool there = row < n_rows;
-      const int qi = there ? row / group : 0, head = g * group + (there ? row % group : 0);
+      const int qi = there ? sh_query[row / group] : 0, head = g * group + (there ? row % group : 0);
       uint32_t f[HD / 16][4];
       float scale, sum;
       load_rows<HD, TQ>(static_cast<const TQ*>(p.q) + (static_cast<size_t>(b) * p.q_rows + qi) * p.ldq + head * HD + t * (HD / 4),
@@ -686,20 +698,42 @@ __global__ void __launch_bounds__(WARPS * 32) score_kv4_kernel(const __grid_cons
       key_scales(page + P::V, t, step, base);
       const int slot0 = (p0 + warp + k * WARPS) * KV4_ROWS;
       const bool whole = slot0 + KV4_ROWS <= all.n;
-      for (int i = 0; i < held; ++i) {
-        uint32_t f[HD / 16][4];
+      // the page's codes, unpacked once for all tiles
+      constexpr int NW = HD / 32;
+      uint32_t codes[2][NW][4];
+      {
+        uint32_t k[2][NW];
 #pragma unroll
-        for (int j = 0; j < HD / 16; ++j)
-          *reinterpret_cast<uint4*>(f[j]) = reinterpret_cast<const uint4*>(smem + S::FRAGS)[(i * (HD / 16) + j) * 32 + lane];
-        float s0[4], s1[4];
-        page_dots<HD>(page, f, r, t, s0, s1);
+        for (int h = 0; h < 2; ++h) {
+          const unsigned char* at = page + (r + 8 * h) * P::ROW + t * 4 * NW;
+          if (NW == 4)
+            *reinterpret_cast<uint4*>(k[h]) = *reinterpret_cast<const uint4*>(at);
+          else
+            *reinterpret_cast<uint2*>(k[h]) = *reinterpret_cast<const uint2*>(at);
+#pragma unroll
+          for (int w = 0; w < NW; ++w) kv4_codes(k[h][w], codes[h][w]);
+        }
+      }
+#pragma unroll 2
+      for (int i = 0; i < held; ++i) {
+        float s[2][4];
+#pragma unroll
+        for (int j = 0; j < HD / 16; ++j) {
+          const uint4 f = reinterpret_cast<const uint4*>(smem + S::FRAGS)[(i * (HD / 16) + j) * 32 + lane];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (j == 0)
+              mma_f16_first(s[h], f.x, f.y, f.z, f.w, codes[h][0][0], codes[h][0][1]);
+            else
+              mma_f16(s[h], f.x, f.y, f.z, f.w, codes[h][j / 2][j % 2 * 2], codes[h][j / 2][j % 2 * 2 + 1]);
+          }
+        }
         const float4 rf = reinterpret_cast<const float4*>(smem + S::ROWF)[i * ROWS + r];
         Seen seen = all;
         if (!whole) seen.local = reinterpret_cast<const unsigned long long*>(smem + S::LOCAL)[i * ROWS + r];
-        const float d[4] = {s0[0] + s0[2], s0[1] + s0[3], s1[0] + s1[2], s1[1] + s1[3]};
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          const float z = fmaf(step[x] * rf.x, d[x], base[x] * rf.y);
+          const float z = fmaf(step[x] * rf.x, s[x / 2][x % 2] + s[x / 2][2 + x % 2], base[x] * rf.y);
           if (rf.w != 0.f && (whole || seen(slot0 + 2 * t + (x & 1) + 8 * (x >> 1)))) sum[x] = fmaf(rf.w, pow2(z - rf.z), sum[x]);
         }
       }
@@ -784,10 +818,8 @@ cudaError_t attention_kv4(const Kv4AttnParams& p, cudaStream_t s) {
 
 cudaError_t kv4_score(const Kv4AttnParams& p, cudaStream_t s) {
   const int bg = p.c.B * p.c.G;
-  int splits = (2 * tc_num_sms() + bg - 1) / bg;
   const int most = (p.c.max_pages + WARPS - 1) / WARPS;
-  splits = splits > most ? most : splits;
-  const dim3 grid(splits, bg);
+  const dim3 grid(std::max(1, std::min(4 * tc_num_sms() / bg, most)), bg);  // four blocks per SM
   if (p.c.hd == 128)
     return p.q_f32 ? launch_sized(score_kv4_kernel<128, float>, ScoreSmem<128>::BYTES, grid, p, s)
                    : launch_sized(score_kv4_kernel<128, bf16>, ScoreSmem<128>::BYTES, grid, p, s);

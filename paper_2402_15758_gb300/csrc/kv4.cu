@@ -29,97 +29,183 @@ struct RowArgs {
   int ldk, ldv, rows;
   const int* slot0;
   const int* counts;
+  int vec;  // rows and their heads start on 16 bytes
 };
 
-// A warp rounds one row of one head, K or V: lane l has channels E l .. E l + E - 1 (E = HD / 32),
-// a minimum and a maximum over the warp, and one store of E codes.
-template <int HD, typename T>
-__global__ void __launch_bounds__(256) kv4_append_kernel(RowArgs a) {
-  pdl_wait();
-  pdl_trigger();
-  constexpr int E = HD / 32;
-  const int lane = threadIdx.x & 31;
-  const long long item = static_cast<long long>(blockIdx.x) * (blockDim.x / 32) + threadIdx.x / 32;
-  const long long items = 2LL * a.c.B * a.rows * a.c.G;
-  if (item >= items) return;
-  const int g = static_cast<int>(item % a.c.G);
-  const int which = static_cast<int>(item / a.c.G % 2);
-  const long long r = item / (2 * a.c.G);
-  const int b = static_cast<int>(r / a.rows), i = static_cast<int>(r % a.rows);
-  if (a.counts && i >= a.counts[b]) return;
-  const T* src = static_cast<const T*>(which ? a.v : a.k) + r * (which ? a.ldv : a.ldk) + g * HD + lane * E;
-  float x[E];
+// Eight consecutive values of a row.
+template <typename T>
+__device__ __forceinline__ void load8(const T* src, bool vec, float (&x)[8]) {
+  if (!vec) {
 #pragma unroll
-  for (int j = 0; j < E; ++j) x[j] = to_f<T>(src[j]);
-  const int slot = a.slot0[b] + i;
-  unsigned char* page = page_of(a.c, b, g, slot);
-  if (!page) return;
+    for (int j = 0; j < 8; ++j) x[j] = to_f<T>(src[j]);
+    return;
+  }
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<float4*>(x) = reinterpret_cast<const float4*>(src)[0];
+    *reinterpret_cast<float4*>(x + 4) = reinterpret_cast<const float4*>(src)[1];
+  } else {
+    const uint4 u = *reinterpret_cast<const uint4*>(src);
+    const uint32_t h[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(h[i] << 16);
+      x[2 * i + 1] = __uint_as_float(h[i] & 0xffff0000u);
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* dst, bool vec, const float (&x)[8]) {
+  if (!vec) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) dst[j] = from_f<T>(x[j]);
+    return;
+  }
+  if constexpr (sizeof(T) == 4) {
+    reinterpret_cast<float4*>(dst)[0] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4*>(dst)[1] = make_float4(x[4], x[5], x[6], x[7]);
+  } else {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+      u[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    *reinterpret_cast<uint4*>(dst) = make_uint4(u[0], u[1], u[2], u[3]);
+  }
+}
+
+// What a thread of the row kernels does: eight channels of one head, K or V, for the two rows of a pair of slots
+// (they share the words of V), as far as both belong to the call.
+template <int HD>
+struct Piece {
+  static constexpr int LANES = HD / 8;  // threads of a row
+  bool any, there[2];
+  int which, slot, part, g;  // slot: of the pair's first row; part: which eight channels
+  long long row[2];          // of k and v
+  unsigned char* page;
+  __device__ __forceinline__ Piece(const RowArgs& a, const Kv4Pool& c, int pairs) {
+    const long long id = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x;
+    part = static_cast<int>(id % LANES);
+    long long i = id / LANES;
+    any = i < 2LL * c.B * pairs * c.G;
+    if (!any) i = 0;
+    g = static_cast<int>(i % c.G);
+    i /= c.G;
+    which = static_cast<int>(i & 1);
+    const int at = static_cast<int>((i >> 1) % pairs), b = static_cast<int>((i >> 1) / pairs);
+    const int s0 = a.slot0[b], count = a.counts ? min(a.counts[b], a.rows) : a.rows;
+    slot = (s0 & ~1) + 2 * at;
+    page = nullptr;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int k = slot + r - s0;
+      there[r] = any && k >= 0 && k < count;
+      row[r] = static_cast<long long>(b) * a.rows + max(k, 0);
+    }
+    if (there[0] || there[1]) page = page_of(c, b, g, slot);
+    if (!page) any = there[0] = there[1] = false;
+  }
+};
+
+// Rounds a row's eight values of this thread: the row's minimum and maximum over its LANES threads, then the codes,
+// four bits each.  A code is rint of the correctly rounded quotient; the product with the reciprocal
+// decides it alone unless it lies within 2^-16 of a tie.
+template <int LANES>
+__device__ __forceinline__ uint32_t round8(const float (&x)[8], uint32_t& scale) {
   float lo = x[0], hi = x[0];
   bool fine = true;
 #pragma unroll
-  for (int j = 0; j < E; ++j) {
+  for (int j = 0; j < 8; ++j) {
     lo = fminf(lo, x[j]);
     hi = fmaxf(hi, x[j]);
     fine = fine && isfinite(x[j]);
   }
 #pragma unroll
-  for (int o = 16; o; o >>= 1) {
+  for (int o = LANES / 2; o; o >>= 1) {
     lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
     hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    fine = __shfl_xor_sync(0xffffffffu, fine, o) && fine;
   }
-  fine = __all_sync(0xffffffffu, fine) && isfinite(hi - lo);
   const bf16 base16 = __float2bfloat16_rn(lo), step16 = __float2bfloat16_rn(__fmul_rn(hi - lo, 1.f / 15.f));
   const float base = __bfloat162float(base16), step = __bfloat162float(step16);
-  fine = fine && isfinite(base);
+  fine = fine && isfinite(hi - lo) && isfinite(base);
+  scale = fine ? __bfloat16_as_ushort(step16) | static_cast<uint32_t>(__bfloat16_as_ushort(base16)) << 16 : 0x7fc00000u;
+  if (!fine || !(step > 0.f)) return 0;
+  const float inv = 1.f / step;
   uint32_t codes = 0;
-  if (fine && step > 0.f) {
 #pragma unroll
-    for (int j = 0; j < E; ++j)
-      codes |= static_cast<uint32_t>(fminf(fmaxf(rintf(__fdiv_rn(x[j] - base, step)), 0.f), 15.f)) << (4 * j);
+  for (int j = 0; j < 8; ++j) {
+    const float d = x[j] - base;
+    float q = d * inv, n = rintf(q);
+    if (!(fabsf(q - n) < 0.5f - 0x1p-16f)) n = rintf(__fdiv_rn(d, step));
+    codes |= static_cast<uint32_t>(fminf(fmaxf(n, 0.f), 15.f)) << (4 * j);
   }
-  const int row = slot % KV4_ROWS;
-  using P = Kv4<HD>;
-  if (E == 4) {
-    unsigned char* at = which ? page + P::v_half(row, lane) : page + row * P::ROW + 2 * lane;
-    *reinterpret_cast<uint16_t*>(at) = static_cast<uint16_t>(codes);
-  } else {
-    unsigned char* at = which ? page + P::v_half(row, lane / 2) + (lane & 1) : page + row * P::ROW + lane;
-    *at = static_cast<unsigned char>(codes);
-  }
-  if (lane == 0) {
-    const uint32_t s16 = fine ? __bfloat16_as_ushort(step16) : 0u, b16 = fine ? __bfloat16_as_ushort(base16) : 0x7fc0u;
-    *reinterpret_cast<uint32_t*>(page + (which ? P::VS : P::KS) + 4 * row) = s16 | b16 << 16;
-  }
+  return codes;
 }
 
 template <int HD, typename T>
-__global__ void __launch_bounds__(256) kv4_read_kernel(RowArgs a) {
+__global__ void __launch_bounds__(256) kv4_append_kernel(RowArgs a, int pairs) {
   pdl_wait();
   pdl_trigger();
-  constexpr int E = HD / 32;
-  const int lane = threadIdx.x & 31;
-  const long long item = static_cast<long long>(blockIdx.x) * (blockDim.x / 32) + threadIdx.x / 32;
-  const long long items = 2LL * a.c.B * a.rows * a.c.G;
-  if (item >= items) return;
-  const int g = static_cast<int>(item % a.c.G);
-  const int which = static_cast<int>(item / a.c.G % 2);
-  const long long r = item / (2 * a.c.G);
-  const int b = static_cast<int>(r / a.rows), i = static_cast<int>(r % a.rows);
-  if (a.counts && i >= a.counts[b]) return;
-  const int slot = a.slot0[b] + i;
-  const unsigned char* page = page_of(a.c, b, g, slot);
-  if (!page) return;
-  const int row = slot % KV4_ROWS;
   using P = Kv4<HD>;
-  uint32_t codes;
-  if (E == 4)
-    codes = *reinterpret_cast<const uint16_t*>(which ? page + P::v_half(row, lane) : page + row * P::ROW + 2 * lane);
-  else
-    codes = *(which ? page + P::v_half(row, lane / 2) + (lane & 1) : page + row * P::ROW + lane);
-  const uint32_t w = *reinterpret_cast<const uint32_t*>(page + (which ? P::VS : P::KS) + 4 * row);
-  T* dst = static_cast<T*>(which ? a.v : a.k) + r * (which ? a.ldv : a.ldk) + g * HD + lane * E;
+  const Piece<HD> w(a, a.c, pairs);
+  float x[2][8];
+  uint32_t codes[2], scale[2];
 #pragma unroll
-  for (int j = 0; j < E; ++j) dst[j] = from_f<T>(fmaf(kv4_step(w), static_cast<float>(codes >> (4 * j) & 15u), kv4_base(w)));
+  for (int r = 0; r < 2; ++r) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[r][j] = 0.f;
+    if (w.there[r])
+      load8<T>(static_cast<const T*>(w.which ? a.v : a.k) + w.row[r] * (w.which ? a.ldv : a.ldk) + w.g * HD + 8 * w.part, a.vec, x[r]);
+  }
+#pragma unroll
+  for (int r = 0; r < 2; ++r) codes[r] = round8<Piece<HD>::LANES>(x[r], scale[r]);
+  if (!w.any) return;
+  const int row = w.slot % KV4_ROWS;
+  if (!w.which) {
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+      if (w.there[r]) *reinterpret_cast<uint32_t*>(w.page + (row + r) * P::ROW + 4 * w.part) = codes[r];
+  } else {
+    unsigned char* at = w.page + P::v_half(row, 2 * w.part);  // words 2 part and 2 part + 1 are neighbours
+    if (w.there[0] && w.there[1]) {
+      *reinterpret_cast<uint2*>(at) = make_uint2(__byte_perm(codes[0], codes[1], 0x5410), __byte_perm(codes[0], codes[1], 0x7632));
+    } else {
+      const int r = w.there[0] ? 0 : 1;
+      *reinterpret_cast<uint16_t*>(at + 2 * r) = static_cast<uint16_t>(codes[r]);
+      *reinterpret_cast<uint16_t*>(at + 2 * r + 4) = static_cast<uint16_t>(codes[r] >> 16);
+    }
+  }
+  if (w.part < 2 && w.there[w.part])
+    *reinterpret_cast<uint32_t*>(w.page + (w.which ? P::VS : P::KS) + 4 * (row + w.part)) = w.part ? scale[1] : scale[0];
+}
+
+template <int HD, typename T>
+__global__ void __launch_bounds__(256) kv4_read_kernel(RowArgs a, int pairs) {
+  pdl_wait();
+  pdl_trigger();
+  using P = Kv4<HD>;
+  const Piece<HD> w(a, a.c, pairs);
+  if (!w.any) return;
+  const int row = w.slot % KV4_ROWS;
+  uint2 c;  // codes of the pair's rows
+  if (!w.which) {
+    c.x = *reinterpret_cast<const uint32_t*>(w.page + row * P::ROW + 4 * w.part);
+    c.y = *reinterpret_cast<const uint32_t*>(w.page + (row + 1) * P::ROW + 4 * w.part);
+  } else {
+    c = *reinterpret_cast<const uint2*>(w.page + P::v_half(row, 2 * w.part));
+    c = make_uint2(__byte_perm(c.x, c.y, 0x5410), __byte_perm(c.x, c.y, 0x7632));
+  }
+  const uint2 scale = *reinterpret_cast<const uint2*>(w.page + (w.which ? P::VS : P::KS) + 4 * row);
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    if (!w.there[r]) continue;
+    const uint32_t codes = r ? c.y : c.x, s = r ? scale.y : scale.x;
+    float x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = fmaf(kv4_step(s), static_cast<float>(codes >> (4 * j) & 15u), kv4_base(s));
+    store8<T>(static_cast<T*>(w.which ? a.v : a.k) + w.row[r] * (w.which ? a.ldv : a.ldk) + w.g * HD + 8 * w.part, a.vec, x);
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -134,38 +220,32 @@ __device__ __forceinline__ uint32_t order_key(float x) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Sum of v over the threads before this one, and the total, for the whole block.
-__device__ __forceinline__ int block_before(int v, int* warp_sums, int& total) {
+constexpr int DIGIT = 11, BINS = 1 << DIGIT;  // 32 bits in three digits (11, 11, 10)
+constexpr int SEL_WARPS = SEL_THREADS / 32, HELD = 16;  // keys that a thread holds in registers
+
+// Sum of v over the warps before this one (a warp's v in any lane), and over all.
+__device__ __forceinline__ int warps_before(int v, int* sums, int& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
-  int x = v;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, x, o);
-    if (lane >= o) x += y;
-  }
   __syncthreads();
-  if (lane == 31) warp_sums[warp] = x;
+  if (lane == 0) sums[warp] = v;
   __syncthreads();
-  int before = 0;
-  total = 0;
-  for (int w = 0; w < SEL_THREADS / 32; ++w) {
-    if (w < warp) before += warp_sums[w];
-    total += warp_sums[w];
-  }
-  return before + x - v;
+  const int x = sums[lane];
+  total = __reduce_add_sync(0xffffffffu, x);
+  return __reduce_add_sync(0xffffffffu, lane < warp ? x : 0);
 }
 
-// One block per (sequence, head): the kept slots.  The (budget - recent)-th largest key of the
-// older slots is found digit by digit (four passes of 8 bits), then one ordered pass takes
-// every slot above it and the first ones that equal it.
+// One block per (sequence, head): the kept slots.  The (budget - recent)-th largest key of the older slots is found
+// digit by digit, three histograms of up to 2048 bins; then one ordered pass takes every slot above it and
+// the first ones that equal it.  A warp owns a contiguous part of the slots, so the order of warps, rounds
+// and lanes is the slots' and the loads are coalesced.
 __global__ void __launch_bounds__(SEL_THREADS) kv4_select_kernel(Kv4EvictParams p) {
   pdl_wait();
   pdl_trigger();
-  __shared__ int hist[256];
-  __shared__ int warp_sums[SEL_THREADS / 32];
-  __shared__ uint32_t sh_prefix;
+  __shared__ int hist[BINS];
+  __shared__ int sums[SEL_WARPS];
+  __shared__ uint32_t sh_digit;
   __shared__ int sh_need;
-  const int bg = blockIdx.x, b = bg / p.c.G, tid = threadIdx.x;
+  const int bg = blockIdx.x, b = bg / p.c.G, tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
   const int cap = min(p.ld_scores, p.c.max_pages * KV4_ROWS);
   int n = p.n_ctx[b];
   if (n < 0 || n > cap) {
@@ -189,104 +269,166 @@ __global__ void __launch_bounds__(SEL_THREADS) kv4_select_kernel(Kv4EvictParams 
     out[want + i] = x[older + i];
   }
   if (want == 0) return;
-  uint32_t prefix = 0;
-  int need = want;  // keys with this prefix that stay
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
+  const int rounds = (older + SEL_THREADS - 1) / SEL_THREADS;  // of a warp, 32 slots each
+  const int begin = warp * rounds * 32 + lane;                 // this thread's first slot
+  float held[HELD];
+#pragma unroll
+  for (int j = 0; j < HELD; ++j) held[j] = j < rounds && begin + 32 * j < older ? x[begin + 32 * j] : 0.f;
+  // f(slot, value, whether there is one), over this warp's slots in order
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int j = 0; j < HELD; ++j)
+      if (j < rounds) f(begin + 32 * j, held[j], begin + 32 * j < older);
+    for (int j = HELD; j < rounds; ++j) {
+      const int i = begin + 32 * j;
+      f(i, i < older ? x[i] : 0.f, i < older);
+    }
+  };
+  uint32_t prefix = 0;  // of the key looked for: the digits found so far
+  int need = want;      // keys with this prefix that stay
+  int width = DIGIT;
+  for (int shift = 32 - DIGIT; shift >= 0; shift -= width) {
+    for (int i = tid; i < BINS; i += SEL_THREADS) hist[i] = 0;
     __syncthreads();
-    for (int i = tid; i < older; i += SEL_THREADS) {
-      const uint32_t key = order_key(x[i]);
-      if (shift == 24 || key >> (shift + 8) == prefix) atomicAdd(&hist[key >> shift & 255], 1);
+    each([&](int, float v, bool there) {
+      const uint32_t key = order_key(v);
+      if (there && (shift + width == 32 || key >> (shift + width) == prefix)) atomicAdd(&hist[key >> shift & ((1u << width) - 1)], 1);
+    });
+    __syncthreads();
+    // thread t has the bins BINS - 1 - 2 t and the one below: counts from the largest digit down
+    const int top = BINS - 1 - 2 * tid, h0 = hist[top], h1 = hist[top - 1];
+    int before = h0 + h1;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, before, o);
+      if (lane >= o) before += y;
+    }
+    int total;
+    before += warps_before(__shfl_sync(0xffffffffu, before, 31), sums, total) - h0 - h1;
+    if (before < need && before + h0 + h1 >= need) {
+      const bool first = before + h0 >= need;
+      sh_digit = first ? top : top - 1;
+      sh_need = need - before - (first ? 0 : h0);
     }
     __syncthreads();
-    if (tid == 0) {
-      int d = 255, left = need;
-      while (d > 0 && hist[d] < left) left -= hist[d--];
-      sh_prefix = prefix << 8 | d;
-      sh_need = left;
-    }
-    __syncthreads();
-    prefix = sh_prefix;
+    prefix = prefix << width | sh_digit;
     need = sh_need;
-    __syncthreads();
+    if (shift == 32 - 2 * DIGIT) width = 32 - 2 * DIGIT;
   }
-  // thread t takes a contiguous part of the older slots, so that the order of threads is the slots'
-  const int per = (older + SEL_THREADS - 1) / SEL_THREADS;
-  const int i0 = min(tid * per, older), i1 = min(i0 + per, older);
+  // slots of this warp above the key, and equal to it
   int above = 0, equal = 0, total;
-  for (int i = i0; i < i1; ++i) {
-    const uint32_t key = order_key(x[i]);
-    above += key > prefix;
-    equal += key == prefix;
-  }
-  int before_equal = block_before(equal, warp_sums, total);
-  const int mine = min(max(need - before_equal, 0), equal);
-  int at = block_before(above + mine, warp_sums, total);
-  int left = mine;
-  for (int i = i0; i < i1; ++i) {
-    const uint32_t key = order_key(x[i]);
-    if (key > prefix || (key == prefix && left-- > 0)) {
-      kept[at] = i;
-      out[at] = x[i];
-      ++at;
+  each([&](int, float v, bool there) {
+    const uint32_t key = order_key(v);
+    above += there && key > prefix;
+    equal += there && key == prefix;
+  });
+  above = __reduce_add_sync(0xffffffffu, above);
+  equal = __reduce_add_sync(0xffffffffu, equal);
+  const int equal_before = warps_before(equal, sums, total);
+  int left = min(max(need - equal_before, 0), equal);  // equal ones that stay
+  int at = warps_before(above + left, sums, total);
+  const uint32_t below = (1u << lane) - 1;
+  each([&](int i, float v, bool there) {
+    const uint32_t key = order_key(v);
+    const uint32_t same = __ballot_sync(0xffffffffu, there && key == prefix);
+    const bool stays = there && (key > prefix || (key == prefix && __popc(same & below) < left));
+    const uint32_t all = __ballot_sync(0xffffffffu, stays);
+    if (stays) {
+      kept[at + __popc(all & below)] = i;
+      out[at + __popc(all & below)] = v;
     }
-  }
+    at += __popc(all);
+    left = max(left - __popc(same), 0);
+  });
 }
 
-// One block per (destination page, sequence and head): gathers the 16 rows kept there.
+// 128 threads per (destination page, sequence and head) gather the 16 rows kept there, 16 bytes a time: a K row's codes
+// as they are, a V chunk from the chunks of its two rows.  Four pages per block.
+constexpr int MOVE_PAGES = 4;
 template <int HD>
-__global__ void __launch_bounds__(128) kv4_move_kernel(Kv4EvictParams p) {
+__global__ void __launch_bounds__(128 * MOVE_PAGES) kv4_move_kernel(Kv4EvictParams p) {
   pdl_wait();
   pdl_trigger();
   using P = Kv4<HD>;
-  const int bg = blockIdx.y, b = bg / p.c.G, g = bg % p.c.G, page = blockIdx.x, tid = threadIdx.x;
-  __shared__ const unsigned char* src[KV4_ROWS];
-  __shared__ int row_of[KV4_ROWS];
-  __shared__ unsigned char* dst;
+  const int bg = blockIdx.y, b = bg / p.c.G, g = bg % p.c.G, tid = threadIdx.x % 128, which = threadIdx.x / 128;
+  const int page = blockIdx.x * MOVE_PAGES + which;
+  __shared__ const unsigned char* sh_src[MOVE_PAGES][KV4_ROWS];
+  __shared__ int sh_row[MOVE_PAGES][KV4_ROWS];
+  __shared__ unsigned char* sh_dst[MOVE_PAGES];
+  const bool used = page * KV4_ROWS < p.budget;
   if (tid < KV4_ROWS) {
     const int i = page * KV4_ROWS + tid;
     const int slot = i < p.budget ? p.kept[static_cast<size_t>(bg) * p.budget + i] : -1;
-    src[tid] = slot >= 0 ? page_of(p.c, b, g, slot) : nullptr;
-    row_of[tid] = slot % KV4_ROWS;
+    sh_src[which][tid] = slot >= 0 ? page_of(p.c, b, g, slot) : nullptr;
+    sh_row[which][tid] = slot & (KV4_ROWS - 1);
   }
   if (tid == KV4_ROWS) {
     Kv4Pool d = p.c;
     d.table = p.dst_table;
     d.max_pages = p.dst_pages;
-    dst = page_of(d, b, g, page * KV4_ROWS);
+    sh_dst[which] = used ? page_of(d, b, g, page * KV4_ROWS) : nullptr;
   }
   __syncthreads();
-  if (!dst || !__syncthreads_or(tid < KV4_ROWS && src[tid])) return;
-  for (int w = tid; w < KV4_ROWS * HD / 8; w += 128) {  // K words
-    const int row = w / (HD / 8), c = w % (HD / 8);
+  unsigned char* dst = sh_dst[which];
+  const unsigned char** src = sh_src[which];
+  const int* row_of = sh_row[which];
+  if (!dst || !src[0]) return;  // (the kept rows come first)
+  if (tid < 64) {
+    // V: pair tid / 8, chunk tid % 8
+    const int pair = tid / 8, chunk = tid % 8;
+    const unsigned char *s0 = src[2 * pair], *s1 = src[2 * pair + 1];
+    if (s0) {
+      const int r0 = row_of[2 * pair], r1 = s1 ? row_of[2 * pair + 1] : 0;
+      const unsigned char* a = s0 + P::V + r0 / 2 * 2 * P::ROW + P::place(r0 / 2, chunk) * P::CHUNK;
+      const unsigned char* c = s1 ? s1 + P::V + r1 / 2 * 2 * P::ROW + P::place(r1 / 2, chunk) * P::CHUNK : a;
+      unsigned char* to = dst + P::V + pair * 2 * P::ROW + P::place(pair, chunk) * P::CHUNK;
+      // halves of the words: row 2 pair from the half of its parity, row 2 pair + 1 likewise
+      const uint32_t pick = (r0 & 1 ? 0x32u : 0x10u) | (r1 & 1 ? 0x7600u : 0x5400u);
+      uint32_t x[P::CHUNK / 4], y[P::CHUNK / 4];
+      if constexpr (HD == 128) {
+        *reinterpret_cast<uint4*>(x) = *reinterpret_cast<const uint4*>(a);
+        *reinterpret_cast<uint4*>(y) = *reinterpret_cast<const uint4*>(c);
+      } else {
+        *reinterpret_cast<uint2*>(x) = *reinterpret_cast<const uint2*>(a);
+        *reinterpret_cast<uint2*>(y) = *reinterpret_cast<const uint2*>(c);
+      }
+#pragma unroll
+      for (int i = 0; i < P::CHUNK / 4; ++i) x[i] = __byte_perm(x[i], y[i], pick);
+      if constexpr (HD == 128)
+        *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(x);
+      else
+        *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(x);
+    }
+    if (tid < 2 * KV4_ROWS) {
+      const int row = tid % KV4_ROWS, at = tid < KV4_ROWS ? P::KS : P::VS;
+      if (src[row])
+        *reinterpret_cast<uint32_t*>(dst + at + 4 * row) = *reinterpret_cast<const uint32_t*>(src[row] + at + 4 * row_of[row]);
+    }
+  } else if (tid - 64 < KV4_ROWS * P::ROW / 16) {
+    const int row = (tid - 64) / (P::ROW / 16), c = (tid - 64) % (P::ROW / 16);
     if (src[row])
-      *reinterpret_cast<uint32_t*>(dst + row * P::ROW + 4 * c) =
-          *reinterpret_cast<const uint32_t*>(src[row] + row_of[row] * P::ROW + 4 * c);
-  }
-  for (int w = tid; w < KV4_ROWS * HD / 4; w += 128) {  // V halfwords
-    const int row = w / (HD / 4), c = w % (HD / 4);
-    if (src[row])
-      *reinterpret_cast<uint16_t*>(dst + P::v_half(row, c)) = *reinterpret_cast<const uint16_t*>(src[row] + P::v_half(row_of[row], c));
-  }
-  if (tid < 2 * KV4_ROWS) {
-    const int row = tid % KV4_ROWS, at = tid < KV4_ROWS ? P::KS : P::VS;
-    if (src[row])
-      *reinterpret_cast<uint32_t*>(dst + at + 4 * row) = *reinterpret_cast<const uint32_t*>(src[row] + at + 4 * row_of[row]);
+      *reinterpret_cast<uint4*>(dst + row * P::ROW + 16 * c) = *reinterpret_cast<const uint4*>(src[row] + row_of[row] * P::ROW + 16 * c);
   }
 }
 
+// The rows of a call lie in rows / 2 + 1 pairs of slots at most, wherever the first one starts.
 template <typename K>
 cudaError_t launch_rows(K kernel, const RowArgs& a, cudaStream_t s) {
-  const long long warps = 2LL * a.c.B * a.rows * a.c.G;
-  if (warps == 0) return cudaSuccess;
-  return launch_pdl(kernel, dim3(static_cast<unsigned>((warps + 7) / 8)), dim3(256), 0, s, a);
+  const int pairs = a.rows / 2 + 1;
+  const long long threads = 2LL * a.c.B * pairs * a.c.G * (a.c.hd / 8);
+  return launch_pdl(kernel, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, s, a, pairs);
+}
+RowArgs row_args(const Kv4Pool& c, void* k, void* v, int f32, int ldk, int ldv, int rows, const int* slot0, const int* counts) {
+  const int wide = f32 ? 4 : 8;  // values in 16 bytes
+  const bool vec = (reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) % 16 == 0 && ldk % wide == 0 && ldv % wide == 0;
+  return RowArgs{c, k, v, ldk, ldv, rows, slot0, counts, vec};
 }
 
 }  // namespace
 
 cudaError_t kv4_append(const Kv4Pool& c, const void* k, const void* v, int f32, int ldk, int ldv, int rows,
                        const int* slot0, const int* counts, cudaStream_t s) {
-  const RowArgs a{c, const_cast<void*>(k), const_cast<void*>(v), ldk, ldv, rows, slot0, counts};
+  const RowArgs a = row_args(c, const_cast<void*>(k), const_cast<void*>(v), f32, ldk, ldv, rows, slot0, counts);
   if (c.hd == 128)
     return f32 ? launch_rows(kv4_append_kernel<128, float>, a, s) : launch_rows(kv4_append_kernel<128, bf16>, a, s);
   return f32 ? launch_rows(kv4_append_kernel<64, float>, a, s) : launch_rows(kv4_append_kernel<64, bf16>, a, s);
@@ -294,7 +436,7 @@ cudaError_t kv4_append(const Kv4Pool& c, const void* k, const void* v, int f32, 
 
 cudaError_t kv4_read(const Kv4Pool& c, void* k, void* v, int f32, int ldk, int ldv, int rows, const int* slot0,
                      const int* counts, cudaStream_t s) {
-  const RowArgs a{c, k, v, ldk, ldv, rows, slot0, counts};
+  const RowArgs a = row_args(c, k, v, f32, ldk, ldv, rows, slot0, counts);
   if (c.hd == 128)
     return f32 ? launch_rows(kv4_read_kernel<128, float>, a, s) : launch_rows(kv4_read_kernel<128, bf16>, a, s);
   return f32 ? launch_rows(kv4_read_kernel<64, float>, a, s) : launch_rows(kv4_read_kernel<64, bf16>, a, s);
@@ -304,9 +446,9 @@ cudaError_t kv4_evict(const Kv4EvictParams& p, cudaStream_t s) {
   const int bg = p.c.B * p.c.G;
   cudaError_t e = launch_pdl(kv4_select_kernel, dim3(bg), dim3(SEL_THREADS), 0, s, p);
   if (e != cudaSuccess) return e;
-  const dim3 grid((p.budget + KV4_ROWS - 1) / KV4_ROWS, bg);
-  return p.c.hd == 128 ? launch_pdl(kv4_move_kernel<128>, grid, dim3(128), 0, s, p)
-                       : launch_pdl(kv4_move_kernel<64>, grid, dim3(128), 0, s, p);
+  const dim3 grid(((p.budget + KV4_ROWS - 1) / KV4_ROWS + MOVE_PAGES - 1) / MOVE_PAGES, bg);
+  return p.c.hd == 128 ? launch_pdl(kv4_move_kernel<128>, grid, dim3(128 * MOVE_PAGES), 0, s, p)
+                       : launch_pdl(kv4_move_kernel<64>, grid, dim3(128 * MOVE_PAGES), 0, s, p);
 }
 
 }  // namespace chimera
