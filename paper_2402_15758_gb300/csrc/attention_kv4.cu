@@ -109,35 +109,6 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// q . c' of 8 rows (hi and lo) with the 16 keys of a page: s0 keys 2t, 2t + 1, s1 keys 8 + those.
-template <int HD>
-__device__ __forceinline__ void page_dots(const unsigned char* page, const uint32_t (&f)[HD / 16][4], int r, int t, float (&s0)[4],
-                                          float (&s1)[4]) {
-  constexpr int NW = HD / 32;  // words of a key per thread
-  const uint32_t* k0 = reinterpret_cast<const uint32_t*>(page + r * Kv4<HD>::ROW) + t * NW;
-  const uint32_t* k1 = k0 + 8 * Kv4<HD>::ROW / 4;
-  uint32_t a[NW], b[NW];
-  if (NW == 4) {
-    *reinterpret_cast<uint4*>(a) = *reinterpret_cast<const uint4*>(k0);
-    *reinterpret_cast<uint4*>(b) = *reinterpret_cast<const uint4*>(k1);
-  } else {
-    *reinterpret_cast<uint2*>(a) = *reinterpret_cast<const uint2*>(k0);
-    *reinterpret_cast<uint2*>(b) = *reinterpret_cast<const uint2*>(k1);
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) s0[i] = s1[i] = 0.f;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    uint32_t u[4];
-    kv4_codes(a[w], u);
-    mma_f16(s0, f[2 * w][0], f[2 * w][1], f[2 * w][2], f[2 * w][3], u[0], u[1]);
-    mma_f16(s0, f[2 * w + 1][0], f[2 * w + 1][1], f[2 * w + 1][2], f[2 * w + 1][3], u[2], u[3]);
-    kv4_codes(b[w], u);
-    mma_f16(s1, f[2 * w][0], f[2 * w][1], f[2 * w][2], f[2 * w][3], u[0], u[1]);
-    mma_f16(s1, f[2 * w + 1][0], f[2 * w + 1][1], f[2 * w + 1][2], f[2 * w + 1][3], u[2], u[3]);
-  }
-}
-
 // (step, base + 8 step) of the keys 2t, 2t + 1, 2t + 8, 2t + 9 of a page.
 __device__ __forceinline__ void key_scales(const unsigned char* at, int t, float (&step)[4], float (&base)[4]) {
   const uint2 a = reinterpret_cast<const uint2*>(at)[t], b = reinterpret_cast<const uint2*>(at)[t + 4];
@@ -204,26 +175,30 @@ __device__ __forceinline__ void store_row(const Kv4AttnParams& p, int bg, int ro
   if (p.lse && lane == 0) p.lse[out * p.H + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
 }
 
-// What a block's warps do: RTW tiles of rows times WARPS / RTW slices of the pages.  PRECISE: tiles of 8 rows in two
-// terms; else 16 rows in one (2^-12 of a query and of a weight, a tenth of the rounding of a bf16 result).
-template <int HD, bool PRECISE, int RTW>
+// What a block's warps do: RTW tiles of rows times WARPS / RTW slices of the pages.  A warp multiplies NM matrices of 16
+// rows with every page that it unpacks: 8 rows in two terms (PRECISE), or 16 in one (2^-12 of a query and of a
+// weight, a tenth of the rounding of a bf16 result).
+template <int HD, bool PRECISE, int NM, int RTW>
 struct Shape {
-  static constexpr int TILE = PRECISE ? 8 : 16, ROWS = TILE * RTW, SLICES = WARPS / RTW;
-  static constexpr int STAGES = 8;  // pages of a slice: four pairs
+  static constexpr int TILE = NM * (PRECISE ? 8 : 16), ROWS = TILE * RTW, SLICES = WARPS / RTW;
+  static constexpr int PAGES = NM == 1 ? 2 : 1;  // of a round: with one matrix two pages, for the overlap
+  static constexpr int STAGES = 6;               // pages of a slice
   static constexpr int RING = STAGES * Kv4<HD>::BYTES;
   static constexpr int PITCH = HD + 8;  // of a row of sums: in the order of the products' columns
   static constexpr int SUMS = WARPS * TILE * PITCH * 4;  // over the rings
   static constexpr int BARS = SLICES * RING > SUMS ? SLICES * RING : SUMS;
   static constexpr int ML = BARS + SLICES * STAGES * 16;  // reference and sum of each warp's rows
-  static constexpr int BYTES = ML + WARPS * TILE * 8;
+  static constexpr int FRAGS = ML + WARPS * TILE * 8;     // NM > 1: the queries, [tile][matrix][HD / 16][lane] 16 bytes
+  static constexpr int BYTES = FRAGS + (NM > 1 ? RTW * NM * (HD / 16) * 512 : 0);
 };
 
-template <int HD, typename TQ, bool PRECISE, int RTW>
-__global__ void __launch_bounds__(WARPS * 32, 3) attn_kv4_kernel(const __grid_constant__ Kv4AttnParams p) {
+template <int HD, typename TQ, bool PRECISE, int NM, int RTW>
+__global__ void __launch_bounds__(WARPS * 32, NM == 1 ? 3 : 2) attn_kv4_kernel(const __grid_constant__ Kv4AttnParams p) {
   extern __shared__ __align__(128) unsigned char smem[];
-  using S = Shape<HD, PRECISE, RTW>;
+  using S = Shape<HD, PRECISE, NM, RTW>;
   using P = Kv4<HD>;
-  constexpr int TILE = S::TILE, NR = PRECISE ? 1 : 2, STAGES = S::STAGES;  // NR: rows of a thread
+  constexpr int TILE = S::TILE, STAGES = S::STAGES, PAGES = S::PAGES, NW = HD / 32;
+  constexpr int RM = PRECISE ? 1 : 2, NR = NM * RM;  // rows of a thread: of a matrix, in all
   __shared__ int sh_abort;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31, r = lane / 4, t = lane & 3;
   const int rt = warp % RTW, slice = warp / RTW;
@@ -252,84 +227,131 @@ __global__ void __launch_bounds__(WARPS * 32, 3) attn_kv4_kernel(const __grid_co
   const int p0 = static_cast<int>(static_cast<long long>(pages) * split / splits);
   const int p1 = static_cast<int>(static_cast<long long>(pages) * (split + 1) / splits);
   const int mine = max(0, (p1 - p0 - slice + S::SLICES - 1) / S::SLICES);
-  const int* table = p.c.table + static_cast<size_t>(b) * p.c.max_pages;
-  int asked = 0;
-  auto request = [&]() {  // one lane: the next page into its place of the ring
-    const int block = block_of(p, table, p0 + slice + asked * S::SLICES), stage = asked % STAGES;
-    mbar_arrive_expect_tx(full + stage, P::BYTES);
-    bulk_load(ring + stage * P::BYTES, p.c.pool + (static_cast<size_t>(block) * p.c.G + g) * P::BYTES, P::BYTES, full + stage);
+  const int* table = p.c.table + static_cast<size_t>(b) * p.c.max_pages + p0 + slice;
+  int asked = 0, ask_stage = 0;
+  uint32_t ask_phase = 1;  // parity of the stage's last release
+  auto request = [&]() {   // one lane: the next page into its place of the ring
+    const int block = block_of(p, table, asked * S::SLICES);
+    mbar_arrive_expect_tx(full + ask_stage, P::BYTES);
+    bulk_load(ring + ask_stage * P::BYTES, p.c.pool + (static_cast<size_t>(block) * p.c.G + g) * P::BYTES, P::BYTES, full + ask_stage);
     ++asked;
+    if (++ask_stage == STAGES) {
+      ask_stage = 0;
+      ask_phase ^= 1;
+    }
   };
   if (lane == 0 && rt == 0)
-    while (asked < min(mine, STAGES - 2)) request();
+    while (asked < min(mine, STAGES - PAGES)) request();
 
-  uint32_t qf[HD / 16][4];
+  uint32_t qf[NM == 1 ? HD / 16 : 1][4];  // with more than one matrix the queries stay in shared memory
+  const uint4* frags = reinterpret_cast<const uint4*>(smem + S::FRAGS) + rt * NM * (HD / 16) * 32 + lane;
   float q_scale[NR], q_sum[NR];
   unsigned long long local[NR];
 #pragma unroll
-  for (int i = 0; i < NR; ++i) {
-    const int row = row0 + rt * TILE + r + 8 * i;
-    const bool there = row < n_rows;
-    const int qi = there ? row / group : 0, head = g * group + (there ? row % group : 0);
-    local[i] = there && p.n_local ? p.anc[p.q_local0 + qi] : 0;
-    const TQ* q = static_cast<const TQ*>(p.q) + (static_cast<size_t>(b) * p.q_rows + qi) * p.ldq + head * HD + t * (HD / 4);
-    if constexpr (PRECISE) {
-      load_rows<HD, TQ>(q, there, p.scale * LOG2E, qf, q_scale[i], q_sum[i]);
-    } else {
-      float x[HD / 4];
-      load_row<HD, TQ>(q, there, p.scale * LOG2E, x, q_scale[i], q_sum[i]);
+  for (int x = 0; x < NM; ++x) {
+    uint32_t f[HD / 16][4];
 #pragma unroll
-      for (int j = 0; j < HD / 16; ++j) {
-        const int at = j / 2 * 8 + 2 * (j & 1);
-        qf[j][i] = pack_f16(x[at], x[at + 4]);
-        qf[j][2 + i] = pack_f16(x[at + 1], x[at + 5]);
+    for (int i = 0; i < RM; ++i) {
+      const int row = row0 + rt * TILE + x * (PRECISE ? 8 : 16) + r + 8 * i;
+      const bool there = row < n_rows;
+      const int qi = there ? row / group : 0, head = g * group + (there ? row % group : 0), at = x * RM + i;
+      local[at] = there && p.n_local ? p.anc[p.q_local0 + qi] : 0;
+      const TQ* q = static_cast<const TQ*>(p.q) + (static_cast<size_t>(b) * p.q_rows + qi) * p.ldq + head * HD + t * (HD / 4);
+      if constexpr (PRECISE) {
+        load_rows<HD, TQ>(q, there, p.scale * LOG2E, f, q_scale[at], q_sum[at]);
+      } else {
+        float v[HD / 4];
+        load_row<HD, TQ>(q, there, p.scale * LOG2E, v, q_scale[at], q_sum[at]);
+#pragma unroll
+        for (int j = 0; j < HD / 16; ++j) {
+          const int c = j / 2 * 8 + 2 * (j & 1);
+          f[j][i] = pack_f16(v[c], v[c + 4]);
+          f[j][2 + i] = pack_f16(v[c + 1], v[c + 5]);
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < HD / 16; ++j) {
+      if constexpr (NM == 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) qf[j][i] = f[j][i];
+      } else if (slice == 0) {
+        const_cast<uint4*>(frags)[(x * (HD / 16) + j) * 32] = make_uint4(f[j][0], f[j][1], f[j][2], f[j][3]);
       }
     }
   }
+  if (NM > 1) __syncthreads();
 
-  float o[HD / 8][4] = {};
+  float o[NM][HD / 8][4] = {};
   float m[NR], l[NR], bs[NR];  // l and bs: this thread's keys alone
 #pragma unroll
   for (int i = 0; i < NR; ++i) m[i] = NONE, l[i] = bs[i] = 0.f;
   float top = 0x1p-126f, inv_top = 0x1p126f;  // power of two above every V step so far
-  // The products of a pair with the queries are taken one pair ahead, so that they overlap the softmax before.
-  int stage = 0;  // of the pair whose products come next
+  int stage = 0;
   uint32_t phase = 0;
-  float dots[2][2][4], ahead[2][2][4];  // [page][keys 0..7, 8..15]
-  bool ok = true;
-  auto products = [&](int k, float (&d)[2][2][4]) {
-    const bool two = k + 1 < mine;
-    ok = mbar_wait_warp(full + stage, phase, &sh_abort, WAIT_NS) && (!two || mbar_wait_warp(full + stage + 1, phase, &sh_abort, WAIT_NS));
-    if (!ok) return;
-    page_dots<HD>(ring + stage * P::BYTES, qf, r, t, d[0][0], d[0][1]);
-    page_dots<HD>(ring + (stage + (two ? 1 : 0)) * P::BYTES, qf, r, t, d[1][0], d[1][1]);
-    stage += 2;
-    if (stage == STAGES) {
-      stage = 0;
-      phase ^= 1;
+  for (int k = 0; k < mine; k += PAGES) {
+    const bool two = PAGES == 2 && k + 1 < mine;
+    if (!mbar_wait_warp(full + stage, phase, &sh_abort, WAIT_NS) ||
+        (two && !mbar_wait_warp(full + stage + 1, phase, &sh_abort, WAIT_NS))) {
+      if (lane == 0) atomicOr(p.c.err, ERR_TIMEOUT);
+      break;
     }
-  };
-  if (mine > 0) products(0, dots);
-  for (int k = 0; ok && k < mine; k += 2) {
-    const bool two = k + 1 < mine;
-    const int now = k % STAGES;  // stage of this pair
-    if (k + 2 < mine) products(k + 2, ahead);
-    if (!ok) break;
-    const unsigned char* page[2] = {ring + now * P::BYTES, ring + (now + (two ? 1 : 0)) * P::BYTES};
-    float z[2][NR][4], step[2][4], base[2][4];
+    const unsigned char* page[PAGES];
+    float z[PAGES][NR][4], step[PAGES][4], base[PAGES][4];
     float zmax[NR], smax = 0.f;
 #pragma unroll
     for (int i = 0; i < NR; ++i) zmax[i] = -INFINITY;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < PAGES; ++h) {
+      page[h] = ring + (stage + (h && two ? 1 : 0)) * P::BYTES;
+      // q . c' of the rows with the 16 keys of the page: s[.][0] keys 2t, 2t + 1, s[.][1] keys 8 + those
+      float s[NM][2][4];
+      uint32_t kw[2][NW];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const unsigned char* at = page[h] + (r + 8 * i) * P::ROW + t * 4 * NW;
+        if (NW == 4)
+          *reinterpret_cast<uint4*>(kw[i]) = *reinterpret_cast<const uint4*>(at);
+        else
+          *reinterpret_cast<uint2*>(kw[i]) = *reinterpret_cast<const uint2*>(at);
+      }
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        uint32_t u[2][4];
+        kv4_codes(kw[0][w], u[0]);
+        kv4_codes(kw[1][w], u[1]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+          for (int x = 0; x < NM; ++x) {
+            uint32_t f[4];
+            if constexpr (NM == 1) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) f[i] = qf[2 * w + j][i];
+            } else {
+              *reinterpret_cast<uint4*>(f) = frags[(x * (HD / 16) + 2 * w + j) * 32];
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              if (w == 0 && j == 0)
+                mma_f16_first(s[x][i], f[0], f[1], f[2], f[3], u[i][2 * j], u[i][2 * j + 1]);
+              else
+                mma_f16(s[x][i], f[0], f[1], f[2], f[3], u[i][2 * j], u[i][2 * j + 1]);
+            }
+          }
+        }
+      }
       key_scales(page[h] + P::KS, t, step[h], base[h]);
 #pragma unroll
-      for (int i = 0; i < NR; ++i) {
+      for (int x = 0; x < NM; ++x) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float* s = dots[h][j / 2];
-          const float d = PRECISE ? s[j % 2] + s[2 + j % 2] : s[2 * i + j % 2];
-          z[h][i][j] = fmaf(step[h][j] * q_scale[i], d, base[h][j] * q_sum[i]);
+        for (int i = 0; i < RM; ++i) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float* d = s[x][j / 2];
+            z[h][x * RM + i][j] = fmaf(step[h][j] * q_scale[x * RM + i], PRECISE ? d[j % 2] + d[2 + j % 2] : d[2 * i + j % 2],
+                                       base[h][j] * q_sum[x * RM + i]);
+          }
         }
       }
       key_scales(page[h] + P::VS, t, step[h], base[h]);
@@ -355,7 +377,7 @@ __global__ void __launch_bounds__(WARPS * 32, 3) attn_kv4_kernel(const __grid_co
     if (__any_sync(0xffffffffu, raise)) {
       float wide = smax;
 #pragma unroll
-      for (int s = 16; s; s >>= 1) wide = fmaxf(wide, __shfl_xor_sync(0xffffffffu, wide, s));
+      for (int x = 16; x; x >>= 1) wide = fmaxf(wide, __shfl_xor_sync(0xffffffffu, wide, x));
       float shrink = 1.f;
       if (wide > top) {
         const uint32_t e = min((__float_as_uint(wide) >> 23) + 1, 252u);
@@ -364,106 +386,110 @@ __global__ void __launch_bounds__(WARPS * 32, 3) attn_kv4_kernel(const __grid_co
         inv_top = __uint_as_float((254 - e) << 23);
         shrink = was * inv_top;
       }
-      float a[NR];
 #pragma unroll
-      for (int i = 0; i < NR; ++i) {
-        const float raised = fmaxf(m[i], quad_max(zmax[i]) - BELOW);
-        a[i] = exp2f(m[i] - raised);
-        m[i] = raised;
-        l[i] *= a[i];
-        bs[i] *= a[i];
-        a[i] *= shrink;
-      }
+      for (int x = 0; x < NM; ++x) {
+        float a[RM];
 #pragma unroll
-      for (int j = 0; j < HD / 8; ++j) {
+        for (int i = 0; i < RM; ++i) {
+          const int at = x * RM + i;
+          const float raised = fmaxf(m[at], quad_max(zmax[at]) - BELOW);
+          a[i] = exp2f(m[at] - raised);
+          m[at] = raised;
+          l[at] *= a[i];
+          bs[at] *= a[i];
+          a[i] *= shrink;
+        }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[j][i] *= a[PRECISE ? 0 : i / 2];
+        for (int j = 0; j < HD / 8; ++j) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[x][j][i] *= a[PRECISE ? 0 : i / 2];
+        }
       }
     }
-    uint32_t wf[2][4];  // the weights as A fragments
+    uint32_t wf[PAGES][NM][4];  // the weights as A fragments
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < PAGES; ++h) {
 #pragma unroll
-      for (int i = 0; i < NR; ++i) {
-        float w[4];
+      for (int x = 0; x < NM; ++x) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float e = pow2(z[h][i][j] - m[i]);
-          l[i] += e;
-          bs[i] = fmaf(e, base[h][j], bs[i]);
-          w[j] = e * (step[h][j] * inv_top);
-        }
-        if (PRECISE) {
-          split_f16(w[0], w[1], wf[h][0], wf[h][1]);
-          split_f16(w[2], w[3], wf[h][2], wf[h][3]);
-        } else {
-          wf[h][i] = pack_f16(w[0], w[1]);
-          wf[h][2 + i] = pack_f16(w[2], w[3]);
+        for (int i = 0; i < RM; ++i) {
+          const int at = x * RM + i;
+          float w[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float e = pow2(z[h][at][j] - m[at]);
+            l[at] += e;
+            bs[at] = fmaf(e, base[h][j], bs[at]);
+            w[j] = e * (step[h][j] * inv_top);
+          }
+          if (PRECISE) {
+            split_f16(w[0], w[1], wf[h][x][0], wf[h][x][1]);
+            split_f16(w[2], w[3], wf[h][x][2], wf[h][x][3]);
+          } else {
+            wf[h][x][i] = pack_f16(w[0], w[1]);
+            wf[h][x][2 + i] = pack_f16(w[2], w[3]);
+          }
         }
       }
     }
     // V: row pairs t and t + 4, channels [CHUNK r, CHUNK (r + 1))
-    constexpr int NV = HD / 32;
-    uint32_t v[2][2][NV];
+    uint32_t v[PAGES][2][NW];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < PAGES; ++h) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const unsigned char* at = page[h] + P::V + (t + 4 * i) * 2 * P::ROW + P::place(t + 4 * i, r) * P::CHUNK;
-        if (NV == 4)
+        if (NW == 4)
           *reinterpret_cast<uint4*>(v[h][i]) = *reinterpret_cast<const uint4*>(at);
         else
           *reinterpret_cast<uint2*>(v[h][i]) = *reinterpret_cast<const uint2*>(at);
       }
     }
 #pragma unroll
-    for (int c = 0; c < NV; ++c) {
-      uint32_t u[4], x[4];
-      float d[4][4];
-      kv4_codes(v[0][0][c], u);
-      kv4_codes(v[0][1][c], x);
+    for (int c = 0; c < NW; ++c) {
+      uint32_t u[PAGES][2][4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        // the tensor cores round their sums toward zero: in a chain over all pages that is a bias
-        if (PRECISE)
-          mma_f16_first(d[i], wf[0][0], wf[0][1], wf[0][2], wf[0][3], u[i], x[i]);
-        else
-          mma_f16(o[4 * c + i], wf[0][0], wf[0][1], wf[0][2], wf[0][3], u[i], x[i]);
+      for (int h = 0; h < PAGES; ++h) {
+        kv4_codes(v[h][0][c], u[h][0]);
+        kv4_codes(v[h][1][c], u[h][1]);
       }
-      kv4_codes(v[1][0][c], u);
-      kv4_codes(v[1][1][c], x);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (PRECISE) {
-          mma_f16(d[i], wf[1][0], wf[1][1], wf[1][2], wf[1][3], u[i], x[i]);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) o[4 * c + i][j] += d[i][j];
-        } else {
-          mma_f16(o[4 * c + i], wf[1][0], wf[1][1], wf[1][2], wf[1][3], u[i], x[i]);
+        for (int x = 0; x < NM; ++x) {
+          float* sum = o[x][4 * c + i];
+          if constexpr (PRECISE) {
+            // the tensor cores round their sums toward zero: in a chain over all pages that would be a bias
+            float d[4];
+            mma_f16_first(d, wf[0][x][0], wf[0][x][1], wf[0][x][2], wf[0][x][3], u[0][0][i], u[0][1][i]);
+            if (PAGES == 2)
+              mma_f16(d, wf[PAGES - 1][x][0], wf[PAGES - 1][x][1], wf[PAGES - 1][x][2], wf[PAGES - 1][x][3], u[PAGES - 1][0][i], u[PAGES - 1][1][i]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum[j] += d[j];
+          } else {
+#pragma unroll
+            for (int h = 0; h < PAGES; ++h)
+              mma_f16(o[x][4 * c + i], wf[h][x][0], wf[h][x][1], wf[h][x][2], wf[h][x][3], u[h][0][i], u[h][1][i]);
+          }
         }
       }
     }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) dots[h][i / 4][i % 4] = ahead[h][i / 4][i % 4];
-    }
     __syncwarp();
-    if (RTW > 1 && lane == 0) {
-      mbar_arrive(empty + now);
-      mbar_arrive(empty + now + 1);
+    if (RTW > 1 && lane < PAGES) mbar_arrive(empty + stage + lane);
+    stage += PAGES;
+    if (stage == STAGES) {
+      stage = 0;
+      phase ^= 1;
     }
-    // the pair after the next two, into the places of the pair before this one
-    if (lane == 0 && rt == 0 && asked < mine) {
-      for (int i = 0; i < 2 && asked < mine; ++i) {
-        const int at = asked % STAGES;
-        if (RTW > 1 && asked >= STAGES && !mbar_wait(empty + at, (asked / STAGES - 1) & 1, &sh_abort, WAIT_NS)) break;
+    // the next pages, into the places of the round before this one
+    if (lane == 0 && rt == 0) {
+      for (int i = 0; i < PAGES && asked < mine; ++i) {
+        if (RTW > 1 && asked >= STAGES && !mbar_wait(empty + ask_stage, ask_phase, &sh_abort, WAIT_NS)) break;
         request();
       }
     }
     __syncwarp();
   }
-  if (!ok && lane == 0) atomicOr(p.c.err, ERR_TIMEOUT);
 
   // the block's sums, over the rings: channel CHUNK n + j of a row at 8 j + n
 #pragma unroll
@@ -477,16 +503,20 @@ __global__ void __launch_bounds__(WARPS * 32, 3) attn_kv4_kernel(const __grid_co
   __syncthreads();
   float* sums = reinterpret_cast<float*>(smem) + warp * TILE * S::PITCH;
 #pragma unroll
-  for (int j = 0; j < HD / 8; ++j) {
+  for (int x = 0; x < NM; ++x) {
 #pragma unroll
-    for (int i = 0; i < NR; ++i)
-      *reinterpret_cast<float2*>(sums + (r + 8 * i) * S::PITCH + 8 * j + 2 * t) =
-          make_float2(fmaf(PRECISE ? o[j][0] + o[j][2] : o[j][2 * i], top, bs[i]),
-                      fmaf(PRECISE ? o[j][1] + o[j][3] : o[j][2 * i + 1], top, bs[i]));
+    for (int j = 0; j < HD / 8; ++j) {
+#pragma unroll
+      for (int i = 0; i < RM; ++i) {
+        const float* d = o[x][j];
+        *reinterpret_cast<float2*>(sums + ((PRECISE ? 8 : 16) * x + r + 8 * i) * S::PITCH + 8 * j + 2 * t) =
+            make_float2(fmaf(PRECISE ? d[0] + d[2] : d[2 * i], top, bs[x * RM + i]), fmaf(PRECISE ? d[1] + d[3] : d[2 * i + 1], top, bs[x * RM + i]));
+      }
+    }
   }
 #pragma unroll
   for (int i = 0; i < NR; ++i)
-    if (t == 0) {
+    if (t == 0) {  // rows r, r + 8, .. of the tile
       ml[(warp * TILE + r + 8 * i) * 2] = m[i];
       ml[(warp * TILE + r + 8 * i) * 2 + 1] = l[i];
     }
@@ -759,19 +789,19 @@ cudaError_t launch_sized(K kernel, size_t smem, dim3 grid, const Kv4AttnParams& 
 
 }  // namespace
 
-// How a call's rows are cut: one term per query where the result is rounded to bf16 alone and there are rows
-// enough to fill its tiles, and warps that share pages when there are several tiles.
+// How a call's rows are cut: one term per query where the result is rounded to bf16 alone and there are rows enough
+// to fill a matrix with them; two matrices per warp from there on; warps that share pages for more rows.
 namespace {
 struct Cut {
   bool precise;
-  int rtw, rows;  // tiles at a time, rows of a block
+  int nm, rtw, rows;  // matrices of a warp, tiles at a time, rows of a block
 };
 Cut cut_of(const Kv4AttnParams& p) {
   const int rows = p.nq * (p.H / p.c.G);
   const bool precise = rows <= 8 || p.out_f32 || p.out_lo || p.lse;
-  const int tile = precise ? 8 : 16, tiles = (rows + tile - 1) / tile;
-  const int rtw = tiles == 1 ? 1 : tiles == 2 ? 2 : 4;
-  return Cut{precise, rtw, tile * rtw};
+  const int matrix = precise ? 8 : 16, nm = rows <= matrix ? 1 : 2;
+  const int rtw = rows <= nm * matrix ? 1 : rows <= 2 * nm * matrix || !precise ? 2 : 4;
+  return Cut{precise, nm, rtw, nm * matrix * rtw};
 }
 int blocks_of(const Kv4AttnParams& p) {
   const Cut c = cut_of(p);
@@ -783,9 +813,9 @@ int kv4_attn_blocks(const Kv4AttnParams& p) { return blocks_of(p); }
 
 int kv4_attn_splits(const Kv4AttnParams& p) {
   const Cut c = cut_of(p);
-  const int blocks = blocks_of(p), pairs = (p.c.max_pages + 2 * WARPS / c.rtw - 1) / (2 * WARPS / c.rtw);
-  const int want = 3 * tc_num_sms() / blocks;  // three blocks per SM, and none left for a second wave
-  return std::max(1, std::min(std::min(want, pairs), 64));
+  const int blocks = blocks_of(p), at_once = WARPS / c.rtw * (c.nm == 1 ? 2 : 1), most = (p.c.max_pages + at_once - 1) / at_once;
+  const int want = (c.nm == 1 ? 3 : 2) * tc_num_sms() / blocks;  // as many as are resident, none left for a second wave
+  return std::max(1, std::min(std::min(want, most), 64));
 }
 
 size_t kv4_attn_ws_floats(const Kv4AttnParams& p) {
@@ -793,21 +823,22 @@ size_t kv4_attn_ws_floats(const Kv4AttnParams& p) {
 }
 
 namespace {
-template <int HD, typename TQ, bool PRECISE, int RTW>
+template <int HD, typename TQ, bool PRECISE, int NM, int RTW>
 cudaError_t launch_attn(const Kv4AttnParams& p, cudaStream_t s) {
+  using S = Shape<HD, PRECISE, NM, RTW>;
   const int blocks = blocks_of(p);
-  const cudaError_t e = launch_sized(attn_kv4_kernel<HD, TQ, PRECISE, RTW>, Shape<HD, PRECISE, RTW>::BYTES, dim3(p.splits, blocks), p, s);
+  const cudaError_t e = launch_sized(attn_kv4_kernel<HD, TQ, PRECISE, NM, RTW>, S::BYTES, dim3(p.splits, blocks), p, s);
   if (e != cudaSuccess || p.splits == 1) return e;
   const long long rows = static_cast<long long>(p.nq) * p.c.B * p.H;
-  return launch_pdl(join_kv4_kernel<HD>, dim3(static_cast<unsigned>(rows)), dim3(128), 0, s, p, Shape<HD, PRECISE, RTW>::ROWS,
-                    blocks / (p.c.B * p.c.G));
+  return launch_pdl(join_kv4_kernel<HD>, dim3(static_cast<unsigned>(rows)), dim3(128), 0, s, p, S::ROWS, blocks / (p.c.B * p.c.G));
 }
 template <int HD, typename TQ>
 cudaError_t launch_cut(const Kv4AttnParams& p, cudaStream_t s) {
   const Cut c = cut_of(p);
-  if (c.precise)
-    return c.rtw == 1 ? launch_attn<HD, TQ, true, 1>(p, s) : c.rtw == 2 ? launch_attn<HD, TQ, true, 2>(p, s) : launch_attn<HD, TQ, true, 4>(p, s);
-  return c.rtw == 1 ? launch_attn<HD, TQ, false, 1>(p, s) : c.rtw == 2 ? launch_attn<HD, TQ, false, 2>(p, s) : launch_attn<HD, TQ, false, 4>(p, s);
+  if (!c.precise)
+    return c.nm == 1 ? launch_attn<HD, TQ, false, 1, 1>(p, s) : c.rtw == 1 ? launch_attn<HD, TQ, false, 2, 1>(p, s) : launch_attn<HD, TQ, false, 2, 2>(p, s);
+  if (c.nm == 1) return launch_attn<HD, TQ, true, 1, 1>(p, s);
+  return c.rtw == 1 ? launch_attn<HD, TQ, true, 2, 1>(p, s) : c.rtw == 2 ? launch_attn<HD, TQ, true, 2, 2>(p, s) : launch_attn<HD, TQ, true, 2, 4>(p, s);
 }
 }  // namespace
 
