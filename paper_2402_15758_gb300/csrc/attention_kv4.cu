@@ -227,20 +227,30 @@ __global__ void __launch_bounds__(WARPS * 32, NM == 1 ? 3 : 2) attn_kv4_kernel(c
   const int p0 = static_cast<int>(static_cast<long long>(pages) * split / splits);
   const int p1 = static_cast<int>(static_cast<long long>(pages) * (split + 1) / splits);
   const int mine = max(0, (p1 - p0 - slice + S::SLICES - 1) / S::SLICES);
+  // The blocks of the next 32 pages, one per lane, and of the 32 after them: a request that read its own table entry
+  // would hold its warp for a trip to L2.
   const int* table = p.c.table + static_cast<size_t>(b) * p.c.max_pages + p0 + slice;
+  auto entries = [&](int k) { return k + lane < mine ? block_of(p, table, (k + lane) * S::SLICES) : 0; };
+  int blocks_now = 0, blocks_next = 0;
+  if (rt == 0) blocks_now = entries(0), blocks_next = entries(32);
   int asked = 0, ask_stage = 0;
   uint32_t ask_phase = 1;  // parity of the stage's last release
-  auto request = [&]() {   // one lane: the next page into its place of the ring
-    const int block = block_of(p, table, asked * S::SLICES);
-    mbar_arrive_expect_tx(full + ask_stage, P::BYTES);
-    bulk_load(ring + ask_stage * P::BYTES, p.c.pool + (static_cast<size_t>(block) * p.c.G + g) * P::BYTES, P::BYTES, full + ask_stage);
-    ++asked;
+  auto request = [&]() {   // the warp: the next page into its place of the ring
+    const int block = __shfl_sync(0xffffffffu, blocks_now, asked & 31);
+    if (lane == 0) {
+      mbar_arrive_expect_tx(full + ask_stage, P::BYTES);
+      bulk_load(ring + ask_stage * P::BYTES, p.c.pool + (static_cast<size_t>(block) * p.c.G + g) * P::BYTES, P::BYTES, full + ask_stage);
+    }
+    if ((++asked & 31) == 0) {
+      blocks_now = blocks_next;
+      blocks_next = entries(asked + 32);
+    }
     if (++ask_stage == STAGES) {
       ask_stage = 0;
       ask_phase ^= 1;
     }
   };
-  if (lane == 0 && rt == 0)
+  if (rt == 0)
     while (asked < min(mine, STAGES - PAGES)) request();
 
   uint32_t qf[NM == 1 ? HD / 16 : 1][4];  // with more than one matrix the queries stay in shared memory
@@ -482,13 +492,12 @@ __global__ void __launch_bounds__(WARPS * 32, NM == 1 ? 3 : 2) attn_kv4_kernel(c
       phase ^= 1;
     }
     // the next pages, into the places of the round before this one
-    if (lane == 0 && rt == 0) {
+    if (rt == 0) {
       for (int i = 0; i < PAGES && asked < mine; ++i) {
-        if (RTW > 1 && asked >= STAGES && !mbar_wait(empty + ask_stage, ask_phase, &sh_abort, WAIT_NS)) break;
+        if (RTW > 1 && asked >= STAGES && !mbar_wait_warp(empty + ask_stage, ask_phase, &sh_abort, WAIT_NS)) break;
         request();
       }
     }
-    __syncwarp();
   }
 
   // the block's sums, over the rings: channel CHUNK n + j of a row at 8 j + n
@@ -683,16 +692,25 @@ __global__ void __launch_bounds__(WARPS * 32) score_kv4_kernel(const __grid_cons
   bool ok = true;
   for (int tile0 = 0; tile0 < tiles; tile0 += SCORE_TILES) {
     const int held = min(SCORE_TILES, tiles - tile0);
-    auto request = [&](int k) {
-      const int block = block_of(p, table, p0 + warp + k * WARPS);
-      uint64_t* bar = bars + (used + k) % STAGES;
-      unsigned char* dst = ring + (used + k) % STAGES * S::PAGE;
-      const unsigned char* src = p.c.pool + (static_cast<size_t>(block) * p.c.G + g) * P::BYTES;
-      mbar_arrive_expect_tx(bar, S::PAGE);
-      bulk_load(dst, src, P::V, bar);
-      bulk_load(dst + P::V, src + P::KS, 4 * KV4_ROWS, bar);
+    // (table entries 32 at a time, one per lane, as in the attention)
+    auto entries = [&](int k) { return k + lane < mine ? block_of(p, table, p0 + warp + (k + lane) * WARPS) : 0; };
+    int blocks_now = entries(0), blocks_next = entries(32);
+    auto request = [&](int k) {  // k counts up from 0
+      const int block = __shfl_sync(0xffffffffu, blocks_now, k & 31);
+      if (lane == 0) {
+        uint64_t* bar = bars + (used + k) % STAGES;
+        unsigned char* dst = ring + (used + k) % STAGES * S::PAGE;
+        const unsigned char* src = p.c.pool + (static_cast<size_t>(block) * p.c.G + g) * P::BYTES;
+        mbar_arrive_expect_tx(bar, S::PAGE);
+        bulk_load(dst, src, P::V, bar);
+        bulk_load(dst + P::V, src + P::KS, 4 * KV4_ROWS, bar);
+      }
+      if ((k & 31) == 31) {
+        blocks_now = blocks_next;
+        blocks_next = entries(k + 33);
+      }
     };
-    if (lane == 0 && ok)
+    if (ok)
       for (int k = 0; k < min(mine, STAGES); ++k) request(k);
     __syncthreads();  // every warp has left the fragments of the tiles before
     for (int i = warp; i < held; i += WARPS) {
@@ -775,7 +793,7 @@ __global__ void __launch_bounds__(WARPS * 32) score_kv4_kernel(const __grid_cons
         if (r == x && slot < all.total && slot < p.ld_scores) scores[slot] += sum[x];
       }
       __syncwarp();
-      if (lane == 0 && k + STAGES < mine) request(k + STAGES);
+      if (k + STAGES < mine) request(k + STAGES);
     }
     used += mine;
   }
