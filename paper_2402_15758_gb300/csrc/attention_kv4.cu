@@ -176,8 +176,9 @@ __device__ __forceinline__ void store_row(const Kv4AttnParams& p, int bg, int ro
 }
 
 // What a block's warps do: RTW tiles of rows times WARPS / RTW slices of the pages.  A warp multiplies NM matrices of 16
-// rows with every page that it unpacks: 8 rows in two terms (PRECISE), or 16 in one (2^-12 of a query and of a
-// weight, a tenth of the rounding of a bf16 result).
+// rows with every page that it unpacks: the hi and lo terms of 8 rows (PRECISE), or 16 rows whose queries take two
+// products and whose weights have one term (2^-12 of a weight, a sixteenth of the rounding of a bf16 result; a
+// query in one term would cost 2^-12 of a logit, which for logits of 20 is as much as that rounding).
 template <int HD, bool PRECISE, int NM, int RTW>
 struct Shape {
   static constexpr int TILE = NM * (PRECISE ? 8 : 16), ROWS = TILE * RTW, SLICES = WARPS / RTW;
@@ -188,8 +189,11 @@ struct Shape {
   static constexpr int SUMS = WARPS * TILE * PITCH * 4;  // over the rings
   static constexpr int BARS = SLICES * RING > SUMS ? SLICES * RING : SUMS;
   static constexpr int ML = BARS + SLICES * STAGES * 16;  // reference and sum of each warp's rows
-  static constexpr int FRAGS = ML + WARPS * TILE * 8;     // NM > 1: the queries, [tile][matrix][HD / 16][lane] 16 bytes
-  static constexpr int BYTES = FRAGS + (NM > 1 ? RTW * NM * (HD / 16) * 512 : 0);
+  // The queries stay in registers, or in shared memory: [tile][matrix][term][HD / 16][lane] 16 bytes.
+  static constexpr bool HELD = PRECISE && NM == 1;
+  static constexpr int TERMS = PRECISE ? 1 : 2;
+  static constexpr int FRAGS = ML + WARPS * TILE * 8;
+  static constexpr int BYTES = FRAGS + (HELD ? 0 : RTW * NM * TERMS * (HD / 16) * 512);
 };
 
 template <int HD, typename TQ, bool PRECISE, int NM, int RTW>
@@ -197,7 +201,7 @@ __global__ void __launch_bounds__(WARPS * 32, NM == 1 ? 3 : 2) attn_kv4_kernel(c
   extern __shared__ __align__(128) unsigned char smem[];
   using S = Shape<HD, PRECISE, NM, RTW>;
   using P = Kv4<HD>;
-  constexpr int TILE = S::TILE, STAGES = S::STAGES, PAGES = S::PAGES, NW = HD / 32;
+  constexpr int TILE = S::TILE, STAGES = S::STAGES, PAGES = S::PAGES, TERMS = S::TERMS, NW = HD / 32;
   constexpr int RM = PRECISE ? 1 : 2, NR = NM * RM;  // rows of a thread: of a matrix, in all
   __shared__ int sh_abort;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31, r = lane / 4, t = lane & 3;
@@ -253,13 +257,13 @@ __global__ void __launch_bounds__(WARPS * 32, NM == 1 ? 3 : 2) attn_kv4_kernel(c
   if (rt == 0)
     while (asked < min(mine, STAGES - PAGES)) request();
 
-  uint32_t qf[NM == 1 ? HD / 16 : 1][4];  // with more than one matrix the queries stay in shared memory
-  const uint4* frags = reinterpret_cast<const uint4*>(smem + S::FRAGS) + rt * NM * (HD / 16) * 32 + lane;
+  uint32_t qf[S::HELD ? HD / 16 : 1][4];
+  uint4* frags = reinterpret_cast<uint4*>(smem + S::FRAGS) + rt * NM * TERMS * (HD / 16) * 32 + lane;
   float q_scale[NR], q_sum[NR];
   unsigned long long local[NR];
 #pragma unroll
   for (int x = 0; x < NM; ++x) {
-    uint32_t f[HD / 16][4];
+    uint32_t f[TERMS][HD / 16][4];
 #pragma unroll
     for (int i = 0; i < RM; ++i) {
       const int row = row0 + rt * TILE + x * (PRECISE ? 8 : 16) + r + 8 * i;
@@ -268,29 +272,32 @@ __global__ void __launch_bounds__(WARPS * 32, NM == 1 ? 3 : 2) attn_kv4_kernel(c
       local[at] = there && p.n_local ? p.anc[p.q_local0 + qi] : 0;
       const TQ* q = static_cast<const TQ*>(p.q) + (static_cast<size_t>(b) * p.q_rows + qi) * p.ldq + head * HD + t * (HD / 4);
       if constexpr (PRECISE) {
-        load_rows<HD, TQ>(q, there, p.scale * LOG2E, f, q_scale[at], q_sum[at]);
+        load_rows<HD, TQ>(q, there, p.scale * LOG2E, f[0], q_scale[at], q_sum[at]);
       } else {
         float v[HD / 4];
         load_row<HD, TQ>(q, there, p.scale * LOG2E, v, q_scale[at], q_sum[at]);
 #pragma unroll
         for (int j = 0; j < HD / 16; ++j) {
           const int c = j / 2 * 8 + 2 * (j & 1);
-          f[j][i] = pack_f16(v[c], v[c + 4]);
-          f[j][2 + i] = pack_f16(v[c + 1], v[c + 5]);
+          split_f16(v[c], v[c + 4], f[0][j][i], f[TERMS - 1][j][i]);
+          split_f16(v[c + 1], v[c + 5], f[0][j][2 + i], f[TERMS - 1][j][2 + i]);
         }
       }
     }
 #pragma unroll
-    for (int j = 0; j < HD / 16; ++j) {
-      if constexpr (NM == 1) {
+    for (int y = 0; y < TERMS; ++y) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) qf[j][i] = f[j][i];
-      } else if (slice == 0) {
-        const_cast<uint4*>(frags)[(x * (HD / 16) + j) * 32] = make_uint4(f[j][0], f[j][1], f[j][2], f[j][3]);
+      for (int j = 0; j < HD / 16; ++j) {
+        if constexpr (S::HELD) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) qf[j][i] = f[y][j][i];
+        } else if (slice == 0) {
+          frags[((x * TERMS + y) * (HD / 16) + j) * 32] = make_uint4(f[y][j][0], f[y][j][1], f[y][j][2], f[y][j][3]);
+        }
       }
     }
   }
-  if (NM > 1) __syncthreads();
+  if (!S::HELD) __syncthreads();
 
   float o[NM][HD / 8][4] = {};
   float m[NR], l[NR], bs[NR];  // l and bs: this thread's keys alone
@@ -334,19 +341,22 @@ __global__ void __launch_bounds__(WARPS * 32, NM == 1 ? 3 : 2) attn_kv4_kernel(c
         for (int j = 0; j < 2; ++j) {
 #pragma unroll
           for (int x = 0; x < NM; ++x) {
-            uint32_t f[4];
-            if constexpr (NM == 1) {
 #pragma unroll
-              for (int i = 0; i < 4; ++i) f[i] = qf[2 * w + j][i];
-            } else {
-              *reinterpret_cast<uint4*>(f) = frags[(x * (HD / 16) + 2 * w + j) * 32];
-            }
+            for (int y = 0; y < TERMS; ++y) {
+              uint32_t f[4];
+              if constexpr (S::HELD) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              if (w == 0 && j == 0)
-                mma_f16_first(s[x][i], f[0], f[1], f[2], f[3], u[i][2 * j], u[i][2 * j + 1]);
-              else
-                mma_f16(s[x][i], f[0], f[1], f[2], f[3], u[i][2 * j], u[i][2 * j + 1]);
+                for (int i = 0; i < 4; ++i) f[i] = qf[2 * w + j][i];
+              } else {
+                *reinterpret_cast<uint4*>(f) = frags[((x * TERMS + y) * (HD / 16) + 2 * w + j) * 32];
+              }
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                if (w == 0 && j == 0 && y == 0)
+                  mma_f16_first(s[x][i], f[0], f[1], f[2], f[3], u[i][2 * j], u[i][2 * j + 1]);
+                else
+                  mma_f16(s[x][i], f[0], f[1], f[2], f[3], u[i][2 * j], u[i][2 * j + 1]);
+              }
             }
           }
         }
@@ -417,6 +427,14 @@ __global__ void __launch_bounds__(WARPS * 32, NM == 1 ? 3 : 2) attn_kv4_kernel(c
       }
     }
     uint32_t wf[PAGES][NM][4];  // the weights as A fragments
+    float inverse[PAGES][4];
+    if (!PRECISE) {
+#pragma unroll
+      for (int h = 0; h < PAGES; ++h) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) inverse[h][j] = __fdividef(1.f, step[h][j] * inv_top);
+      }
+    }
 #pragma unroll
     for (int h = 0; h < PAGES; ++h) {
 #pragma unroll
@@ -424,13 +442,11 @@ __global__ void __launch_bounds__(WARPS * 32, NM == 1 ? 3 : 2) attn_kv4_kernel(c
 #pragma unroll
         for (int i = 0; i < RM; ++i) {
           const int at = x * RM + i;
-          float w[4];
+          float e[4], w[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const float e = pow2(z[h][at][j] - m[at]);
-            l[at] += e;
-            bs[at] = fmaf(e, base[h][j], bs[at]);
-            w[j] = e * (step[h][j] * inv_top);
+            e[j] = pow2(z[h][at][j] - m[at]);
+            w[j] = e[j] * (step[h][j] * inv_top);
           }
           if (PRECISE) {
             split_f16(w[0], w[1], wf[h][x][0], wf[h][x][1]);
@@ -438,6 +454,19 @@ __global__ void __launch_bounds__(WARPS * 32, NM == 1 ? 3 : 2) attn_kv4_kernel(c
           } else {
             wf[h][x][i] = pack_f16(w[0], w[1]);
             wf[h][x][2 + i] = pack_f16(w[2], w[3]);
+            // The sums take the weights as they were rounded: the row stays an average of its values, and a key that
+            // takes nearly all of it gives its value without the rounding.
+            const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&wf[h][x][i]));
+            const float2 c = __half22float2(*reinterpret_cast<const __half2*>(&wf[h][x][2 + i]));
+            const float rounded[4] = {a.x, a.y, c.x, c.y};
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (step[h][j] * inv_top > 0x1p-100f) e[j] = rounded[j] * inverse[h][j];
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            l[at] += e[j];
+            bs[at] = fmaf(e[j], base[h][j], bs[at]);
           }
         }
       }
@@ -807,7 +836,7 @@ cudaError_t launch_sized(K kernel, size_t smem, dim3 grid, const Kv4AttnParams& 
 
 }  // namespace
 
-// How a call's rows are cut: one term per query where the result is rounded to bf16 alone and there are rows enough
+// How a call's rows are cut: one term per weight where the result is rounded to bf16 alone and there are rows enough
 // to fill a matrix with them; two matrices per warp from there on; warps that share pages for more rows.
 namespace {
 struct Cut {
