@@ -828,10 +828,10 @@ __global__ void __launch_bounds__(WARPS * 32) score_kv4_kernel(const __grid_cons
   }
 }
 
-template <typename K>
-cudaError_t launch_sized(K kernel, size_t smem, dim3 grid, const Kv4AttnParams& p, cudaStream_t s) {
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-  return e != cudaSuccess ? e : launch_pdl(kernel, grid, dim3(WARPS * 32), smem, s, p);
+template <auto KERNEL>
+cudaError_t launch_sized(size_t smem, dim3 grid, const Kv4AttnParams& p, cudaStream_t s) {
+  const cudaError_t e = allow_smem<KERNEL>(smem);
+  return e != cudaSuccess ? e : launch_pdl(KERNEL, grid, dim3(WARPS * 32), smem, s, p);
 }
 
 }  // namespace
@@ -874,7 +874,7 @@ template <int HD, typename TQ, bool PRECISE, int NM, int RTW>
 cudaError_t launch_attn(const Kv4AttnParams& p, cudaStream_t s) {
   using S = Shape<HD, PRECISE, NM, RTW>;
   const int blocks = blocks_of(p);
-  const cudaError_t e = launch_sized(attn_kv4_kernel<HD, TQ, PRECISE, NM, RTW>, S::BYTES, dim3(p.splits, blocks), p, s);
+  const cudaError_t e = launch_sized<attn_kv4_kernel<HD, TQ, PRECISE, NM, RTW>>(S::BYTES, dim3(p.splits, blocks), p, s);
   if (e != cudaSuccess || p.splits == 1) return e;
   const long long rows = static_cast<long long>(p.nq) * p.c.B * p.H;
   return launch_pdl(join_kv4_kernel<HD>, dim3(static_cast<unsigned>(rows)), dim3(128), 0, s, p, S::ROWS, blocks / (p.c.B * p.c.G));
@@ -899,10 +899,10 @@ cudaError_t kv4_score(const Kv4AttnParams& p, cudaStream_t s) {
   const int most = (p.c.max_pages + WARPS - 1) / WARPS;
   const dim3 grid(std::max(1, std::min(4 * tc_num_sms() / bg, most)), bg);  // four blocks per SM
   if (p.c.hd == 128)
-    return p.q_f32 ? launch_sized(score_kv4_kernel<128, float>, ScoreSmem<128>::BYTES, grid, p, s)
-                   : launch_sized(score_kv4_kernel<128, bf16>, ScoreSmem<128>::BYTES, grid, p, s);
-  return p.q_f32 ? launch_sized(score_kv4_kernel<64, float>, ScoreSmem<64>::BYTES, grid, p, s)
-                 : launch_sized(score_kv4_kernel<64, bf16>, ScoreSmem<64>::BYTES, grid, p, s);
+    return p.q_f32 ? launch_sized<score_kv4_kernel<128, float>>(ScoreSmem<128>::BYTES, grid, p, s)
+                   : launch_sized<score_kv4_kernel<128, bf16>>(ScoreSmem<128>::BYTES, grid, p, s);
+  return p.q_f32 ? launch_sized<score_kv4_kernel<64, float>>(ScoreSmem<64>::BYTES, grid, p, s)
+                 : launch_sized<score_kv4_kernel<64, bf16>>(ScoreSmem<64>::BYTES, grid, p, s);
 }
 
 }  // namespace chimera

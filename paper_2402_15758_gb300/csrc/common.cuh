@@ -282,6 +282,11 @@ __device__ __forceinline__ void tma_prefetch_2d(const CUtensorMap* map, int c0, 
                : "memory");
 }
 
+// Bulk request of `bytes` (a multiple of 16) at p into L2.
+__device__ __forceinline__ void prefetch_l2(const void* p, uint32_t bytes) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(__cvta_generic_to_global(p)), "r"(bytes) : "memory");
+}
+
 // Reductions into global memory that return nothing (red, not atom): the issuing thread
 // never waits for them.
 __device__ __forceinline__ void red_add_f32(float* addr, float v) {

@@ -16,6 +16,8 @@
 
 #include <cuda_runtime.h>
 
+#include <atomic>
+
 namespace chimera {
 
 template <typename... KArgs, typename... Args>
@@ -32,6 +34,20 @@ inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, s
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
+}
+
+// Lets a kernel have `bytes` of dynamic shared memory, asked for once per device: the call costs about what a
+// launch does.
+template <auto KERNEL>
+inline cudaError_t allow_smem(size_t bytes) {
+  constexpr int DEVICES = 64;
+  static std::atomic<bool> allowed[DEVICES];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || (dev < DEVICES && allowed[dev].load(std::memory_order_relaxed))) return e;
+  e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+  if (e == cudaSuccess && dev < DEVICES) allowed[dev].store(true, std::memory_order_relaxed);
+  return e;
 }
 
 }  // namespace chimera

@@ -1,16 +1,10 @@
 // Linear with 4-bit weights: Y[M][N] (epilogue)= X[M][K] . W^T with
 // W[n][k] = scale[n][k / group] (code[n][k] - zero[n][k / group]), codes 0..15.
 //
-// code - zero is a whole number of at most 4 bits and a sign, exact in bf16, so a group's
-// products with bf16 activations are exact and are summed in fp32 by the matrix units;
-// the group's scale multiplies the sum, in fp32.  fp32 activations enter as three bf16 terms
-// (24 bits), hi + lo ones as their two.
-//
-// The weights are the A operand (16 features) straight from the packed words: thread
-// (r, t) of a warp takes the word of 8 codes at t of a 32-code block of features r and r + 8, and
-// the activations are staged in shared memory in the order in which the nibbles come out.  Eight
-// warps share 16 features, each with every eighth block of K, and their sums are added
-// in the order of the warps.
+// A group's products are summed in fp32 by the matrix units; what its zero takes off and its scale follow in fp32,
+// from the group's sum of the activations:
+//   Y[m][n] = sum over groups of scale (sum code X - zero sum X).
+// The activations enter as fp16, scaled by a power of two per token, hi + lo or fp32 ones as two fp16 terms (2^-23).
 #include <algorithm>
 
 #include "kernels.h"
@@ -21,29 +15,31 @@
 namespace chimera {
 namespace {
 
-constexpr int WARPS = 8, FEATURES = 16;
+constexpr int WARPS = 24, THREADS = WARPS * 32, FEATURES = 16;
 // ---------------------------------------------------------------------------
 // up to 8 tokens: one pass over the weights at the speed of memory
 // ---------------------------------------------------------------------------
-// A tile is 16 features; KS warps of a CTA share its K, by spans of four groups, and join their sums after
-// JOIN tiles or at the end.  A lane copies (cp.async) into shared memory exactly what it will read itself, so a
-// warp runs ahead of its loads with no barrier at all.  The activations stay in shared memory for
-// the whole launch, as fp16 scaled by a power of two, hi + lo or fp32 ones as two fp16 terms
-// (2^-23).  fp16 rather than bf16 because its ten bits of mantissa take a nibble in two
-// places: 9 instructions for 8 codes, not 11.
+// One CTA of 24 warps per SM.  A tile is 16 features (the MMA's rows); KS warps share its K by spans of four groups
+// and join their sums after `join` tiles or at the end.  A lane copies (cp.async) into shared memory exactly what it
+// will read itself, so a warp runs ahead of its loads with no barrier at all.  The activations stay in shared memory
+// for the whole launch.  A nibble is used where it lies: at the end of a mantissa with exponent 0 it is a (subnormal)
+// fp16 number, so 8 codes cost 5 instructions; nibbles at bit 4 count 16 times, in sums of their own.
 //
-// Measured (GB300, 22016 x 4096, group 128, one token, 47 MB): 16.3 us, 2.9 TB/s; the first kernel of this
-// file 40.  Rings of bulk copies of 256 to 1024 bytes took 19.5 to 23, spans held in registers 17.7 (16
-// warps per SM instead of 24).  Bound by the instructions that turn codes into numbers.
-constexpr int FEW_TOKENS = 8, JOIN = 8;
+// Measured (GB300, 22016 x 4096, group 128, 47 MB): one token 14.4 us, 3.3 TB/s; 8 tokens 18.8; 4096 x 4096 5.9 us.
+// With codes converted to fp16 numbers (9 instructions) 15.2; with three CTAs of 8 warps, each with its own copy
+// of the activations, 14.8, 8 tokens 23 to 26, 4096 x 4096 6.7.  Rings of bulk copies of 256 to 1024 bytes took 19.5
+// to 23, spans held in registers 17.7.  About 4.5 us of every call are the launch, the activations and the join;
+// the rest is bound by instructions and memory alike.
+constexpr int FEW_TOKENS = 8;
 
 struct FewParams {
   W4Params w;
   int groups, spans, tiles, ks;
   int stages;          // of a warp's ring
+  int join;            // tiles whose sums are held
   int x_pitch;         // of a token's term
   int pairs;           // ceil(M / 2): lanes of a row that hold tokens
-  int at_x, at_sums;   // offsets in shared memory
+  int at_x, at_sums_x, at_sums;   // offsets in shared memory
 };
 
 // The scale of a token whose largest magnitude is 2^-6 to 2^7 is 2^8 without asking, so one pass over
@@ -65,6 +61,19 @@ struct Rows {
   __device__ __forceinline__ Rows(const FewParams& p, int tile, int r)
       : a(min(tile * FEATURES + r, p.w.N - 1)), b(min(tile * FEATURES + r + 8, p.w.N - 1)) {}
 };
+
+// The eight codes of a word in pairs (0,4), (1,5), (2,6), (3,7) as the smallest fp16 numbers, without a conversion: a
+// nibble c at the end of a mantissa with exponent 0 is c CODE_UNIT, one at bit 4 is 16 c CODE_UNIT.
+constexpr float CODE_UNIT = 1.f / 16777216.f;
+__device__ __forceinline__ void codes_tiny(uint32_t w, uint32_t (&u)[4]) {
+  const uint32_t h = w >> 8;
+  u[0] = w & 0x000f000fu;
+  u[1] = w & 0x00f000f0u;
+  u[2] = h & 0x000f000fu;
+  u[3] = h & 0x00f000f0u;
+}
+__device__ __forceinline__ uint32_t bf16_bits(uint32_t z) { return __float_as_uint(static_cast<float>(z)) & 0xffff0000u; }
+__device__ __forceinline__ float2 half2_f(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2*>(&h)); }
 
 // Copies a lane's share of one stage: what a lane copies it alone reads, so the ring needs no barrier.
 template <int G>
@@ -108,20 +117,23 @@ __device__ __forceinline__ void swap_near(uint4& v, int t) {
 }
 
 template <int G, int TERMS>
-__global__ void __launch_bounds__(WARPS * 32, 3) w4_few_kernel(const __grid_constant__ FewParams p) {
+__global__ void __launch_bounds__(THREADS, 1) w4_few_kernel(const __grid_constant__ FewParams p) {
   extern __shared__ __align__(128) unsigned char smem[];  // the warps' rings, activations, sums
   __shared__ uint32_t sh_top[FEW_TOKENS];
   constexpr int BLOCKS = Span<G>::BLOCKS;
   const W4Params& w = p.w;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid & 31, r = lane / 4, t = lane & 3;
+  // this warp's stream: spans part, part + KS, .. of tiles first, first + step, ..
+  const int part = warp % p.ks, per_cta = WARPS / p.ks, step = gridDim.x * per_cta;
+  const int first = blockIdx.x + warp / p.ks * gridDim.x;
+  // The launch before may still be writing the weights, so what comes first is only asked into L2.
+  if (part == 0 && lane < FEATURES && first < p.tiles)
+    prefetch_l2(w.W + static_cast<size_t>(min(first * FEATURES + lane, w.N - 1)) * (w.K / 2), w.K / 2);
   if (tid < FEW_TOKENS) sh_top[tid] = 0;
   __syncthreads();
   pdl_wait();
   pdl_trigger();
 
-  // this warp's stream: spans part, part + KS, .. of tiles first, first + step, ..
-  const int part = warp % p.ks, per_cta = WARPS / p.ks, step = gridDim.x * per_cta;
-  const int first = blockIdx.x * per_cta + warp / p.ks;
   unsigned char* ring = smem + warp * p.stages * Span<G>::STAGE + lane * 16;
   int ask_tile = first, ask_span = part, ask_sub = 0, ask_stage = 0;  // the next stage to copy
   auto ask = [&]() {
@@ -146,38 +158,73 @@ __global__ void __launch_bounds__(WARPS * 32, 3) w4_few_kernel(const __grid_cons
   // The activations, in the order in which the codes are multiplied: 128-column block, word of a thread,
   // thread, 8 values; zeros past the end.
   const int vecs = p.spans * 4 * G / 8;
-  auto convert = [&](int m, float up, bool look) {
-    uint32_t top = 0;
-    for (int i = tid; i < vecs; i += WARPS * 32) {
-      float x[8] = {};
-      if (8 * i < w.K) load8(w, m, 8 * i, x);
-      top = max(top, top_bits(x));
-      uint32_t hi[4], lo[4];
+  float* sums_x = reinterpret_cast<float*>(smem + p.at_sums_x);  // [group][token]
+  auto place = [&](int m, int i, const float (&x)[8], float up) {
+    uint32_t hi[4], lo[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) split_f16(x[j] * up, x[j + 4] * up, hi[j], lo[j]);
-      const int from = i / 4 % 4, word = i % 4;  // the lane that loads this word, and its place there
-      int th, at;                                // the lane that multiplies it, and its place there
-      if (G == 128) {
-        th = from, at = word;
-      } else if (G == 64) {
-        th = (from & 1) | (word & 2), at = (from & 2) | (word & 1);
-      } else {
-        th = word, at = from;
-      }
-      unsigned char* dst = smem + p.at_x + m * TERMS * p.x_pitch + i / 16 * 256 + (at * 4 + th) * 16;
-      *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-      if (TERMS == 2) *reinterpret_cast<uint4*>(dst + p.x_pitch) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    for (int j = 0; j < 4; ++j) split_f16(x[j] * up, x[j + 4] * up, hi[j], lo[j]);
+    const int from = i / 4 % 4, word = i % 4;  // the lane that loads this word, and its place there
+    int th, at;                                // the lane that multiplies it, and its place there
+    if (G == 128) {
+      th = from, at = word;
+    } else if (G == 64) {
+      th = (from & 1) | (word & 2), at = (from & 2) | (word & 1);
+    } else {
+      th = word, at = from;
     }
-    if (!look) return;
-    top = __reduce_max_sync(0xffffffffu, top);
-    if (lane == 0) atomicMax(sh_top + m, top);
+    unsigned char* dst = smem + p.at_x + m * TERMS * p.x_pitch + i / 16 * 256 + (at * 4 + th) * 16;
+    *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    if (TERMS == 2) *reinterpret_cast<uint4*>(dst + p.x_pitch) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    // the group's sum, of what the matrix units will be given
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float2 f = half2_f(hi[j]);
+      sum += f.x + f.y;
+      if (TERMS == 2) {
+        f = half2_f(lo[j]);
+        sum += f.x + f.y;
+      }
+    }
+    constexpr int LANES = G / 8;
+    const uint32_t mask = ((1u << LANES) - 1u) << (lane & -LANES);
+#pragma unroll
+    for (int d = 1; d < LANES; d *= 2) sum += __shfl_xor_sync(mask, sum, d);
+    if (lane % LANES == 0) sums_x[i / LANES * FEW_TOKENS + m] = sum * CODE_UNIT;
   };
-  for (int m = 0; m < w.M; ++m) convert(m, USUAL_SCALE, true);
+  // all tokens' in one sequence, AHEAD loads of a thread in flight
+  constexpr int AHEAD = 2;
+  for (int q0 = tid; q0 - lane < w.M * vecs; q0 += AHEAD * THREADS) {
+    float x[AHEAD][8];
+    int m[AHEAD], i[AHEAD];
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      const int q = q0 + a * THREADS;
+      m[a] = q / vecs;
+      i[a] = q - m[a] * vecs;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[a][j] = 0.f;
+      if (m[a] < w.M && 8 * i[a] < w.K) load8(w, m[a], 8 * i[a], x[a]);
+    }
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      const bool there = m[a] < w.M;
+      if (there) place(m[a], i[a], x[a], USUAL_SCALE);
+      const uint32_t mask = vecs % 32 == 0 ? 0xffffffffu : 0xffffu << (lane & 16);
+      const uint32_t top = __reduce_max_sync(mask, there ? top_bits(x[a]) : 0u);
+      if (there && (lane & (vecs % 32 == 0 ? 31 : 15)) == 0) atomicMax(sh_top + m[a], top);
+    }
+  }
   __syncthreads();
   bool again = false;
   for (int m = 0; m < w.M; ++m)
     if (!usual(sh_top[m])) {
-      convert(m, token_scale(sh_top[m]), false);
+      const float up = token_scale(sh_top[m]);
+      for (int i = tid; i < vecs; i += THREADS) {
+        float x[8] = {};
+        if (8 * i < w.K) load8(w, m, 8 * i, x);
+        place(m, i, x, up);
+      }
       again = true;
     }
   if (again) __syncthreads();
@@ -190,12 +237,18 @@ __global__ void __launch_bounds__(WARPS * 32, 3) w4_few_kernel(const __grid_cons
 
   // columns past the last token repeat it, and are not stored
   const unsigned char* xs = smem + p.at_x + min(r, w.M - 1) * TERMS * p.x_pitch + t * 16;
-  float4* sums = reinterpret_cast<float4*>(smem + p.at_sums);  // [JOIN tiles][warp][row][pair of tokens]
+  float4* sums = reinterpret_cast<float4*>(smem + p.at_sums);  // [tile][warp][row][pair of tokens]
   const int mine = r * p.pairs + t, line = 8 * p.pairs;
   int held = 0, first_tile = first;  // tiles whose sums are held, the first of them
   // joins the sums of the held tiles: warp j of the KS takes tiles j, j + KS, ..
+  auto meet = [&]() {  // of the warps that share tiles
+    if (p.ks > 1)
+      named_bar(1 + warp / p.ks, p.ks * 32);
+    else
+      __syncwarp();
+  };
   auto join = [&]() {
-    named_bar(1 + warp / p.ks, p.ks * 32);
+    meet();
     for (int j = part; j < held && t < p.pairs; j += p.ks) {
       const float4* from = sums + (j * WARPS + warp - part) * line + mine;
       float4 y = from[0];
@@ -207,9 +260,9 @@ __global__ void __launch_bounds__(WARPS * 32, 3) w4_few_kernel(const __grid_cons
       const float v[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (2 * t + (i & 1) < w.M && n + 8 * (i >> 1) < w.N) store_y(w, 2 * t + (i & 1), n + 8 * (i >> 1), v[i] * down[i & 1]);
+        if (2 * t + (i & 1) < w.M && n + 8 * (i >> 1) < w.N) store_y(w, 2 * t + (i & 1), n + 8 * (i >> 1), v[i] * (1.f / CODE_UNIT) * down[i & 1]);
     }
-    named_bar(1 + warp / p.ks, p.ks * 32);
+    meet();
     first_tile += held * step;
     held = 0;
   };
@@ -239,48 +292,50 @@ __global__ void __launch_bounds__(WARPS * 32, 3) w4_few_kernel(const __grid_cons
         if (G < 128) swap_far(va, t), swap_far(vb, t);
         if (G < 64) swap_near(va, t), swap_near(vb, t);
         const uint32_t a[4] = {va.x, va.y, va.z, va.w}, b[4] = {vb.x, vb.y, vb.z, vb.w};
-        const uint32_t both_a = now.sa | now.za << 16, both_b = now.sb | now.zb << 16;
-        uint32_t oa, oa16, ob, ob16;
-        float sa, sb, d[4];
+        const uint32_t both_a = bf16_bits(now.za) | now.sa, both_b = bf16_bits(now.zb) | now.sb;
+        float sa, sb, za, zb, low[4], high[4];  // products of the low and the high nibbles of a group's bytes
+        float2 sum_x;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
           if (v % BLOCKS == 0) {  // a new group
             const int g = i * (4 / BLOCKS) + v / BLOCKS;
             const uint32_t ga = __shfl_sync(0xffffffffu, both_a, (lane & ~3) | g), gb = __shfl_sync(0xffffffffu, both_b, (lane & ~3) | g);
-            oa = zero_off(ga >> 16), oa16 = zero_off16(ga >> 16), ob = zero_off(gb >> 16), ob16 = zero_off16(gb >> 16);
             sa = __uint_as_float(ga << 16), sb = __uint_as_float(gb << 16);
+            za = __uint_as_float(ga & 0xffff0000u), zb = __uint_as_float(gb & 0xffff0000u);
+            sum_x = *reinterpret_cast<const float2*>(sums_x + (span * 4 + g) * FEW_TOKENS + 2 * t);
           }
           uint32_t ua[4], ub[4];
-          w4_codes_f16(a[v], oa, oa16, ua);
-          w4_codes_f16(b[v], ob, ob16, ub);
+          codes_tiny(a[v], ua);
+          codes_tiny(b[v], ub);
 #pragma unroll
           for (int s = 0; s < TERMS; ++s) {
             const uint4 x = *reinterpret_cast<const uint4*>(xb + i * 256 + s * p.x_pitch + v * 64);
-            if (v % BLOCKS == 0 && s == 0)
-              mma_f16_first(d, ua[0], ub[0], ua[1], ub[1], x.x, x.y);
-            else
-              mma_f16(d, ua[0], ub[0], ua[1], ub[1], x.x, x.y);
-            mma_f16(d, ua[2], ub[2], ua[3], ub[3], x.z, x.w);
+            if (v % BLOCKS == 0 && s == 0) {
+              mma_f16_first(low, ua[0], ub[0], ua[2], ub[2], x.x, x.z);
+              mma_f16_first(high, ua[1], ub[1], ua[3], ub[3], x.y, x.w);
+            } else {
+              mma_f16(low, ua[0], ub[0], ua[2], ub[2], x.x, x.z);
+              mma_f16(high, ua[1], ub[1], ua[3], ub[3], x.y, x.w);
+            }
           }
           if (v % BLOCKS == BLOCKS - 1) {
-            acc[0] = fmaf(sa, d[0], acc[0]);
-            acc[1] = fmaf(sa, d[1], acc[1]);
-            acc[2] = fmaf(sb, d[2], acc[2]);
-            acc[3] = fmaf(sb, d[3], acc[3]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              acc[j] = fmaf(j < 2 ? sa : sb, fmaf(high[j], 0.0625f, fmaf(j < 2 ? -za : -zb, j & 1 ? sum_x.y : sum_x.x, low[j])), acc[j]);
           }
         }
       }
     }
     if (t < p.pairs) sums[(held * WARPS + warp) * line + mine] = make_float4(acc[0], acc[1], acc[2], acc[3]);
-    if (++held == JOIN) join();
+    if (++held == p.join) join();
   }
   if (held) join();
 }
 
 template <int G, int TERMS>
 cudaError_t launch_few(const FewParams& p, size_t smem, int grid, cudaStream_t s) {
-  const cudaError_t e = cudaFuncSetAttribute(w4_few_kernel<G, TERMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024);
-  return e != cudaSuccess ? e : launch_pdl(w4_few_kernel<G, TERMS>, dim3(grid), dim3(WARPS * 32), smem, s, p);
+  const cudaError_t e = allow_smem<w4_few_kernel<G, TERMS>>(226 * 1024);
+  return e != cudaSuccess ? e : launch_pdl(w4_few_kernel<G, TERMS>, dim3(grid), dim3(THREADS), smem, s, p);
 }
 template <int G>
 cudaError_t launch_few_terms(const FewParams& p, size_t smem, int grid, cudaStream_t s) {
@@ -296,32 +351,29 @@ size_t few_plan(FewParams* p, const W4Params& w, int* grid) {
   p->x_pitch = p->spans * 4 * w.group * 2 + 64;  // two tokens' reads in different banks
   const int terms = w.x_f32 || w.X_lo ? 2 : 1, stage = WARPS * (w.group == 32 ? 1024 : 2048);
   p->pairs = (w.M + 1) / 2;
-  const int x_bytes = (w.M * terms * p->x_pitch + 127) / 128 * 128, sums = JOIN * WARPS * 8 * p->pairs * 16;
-  int per_sm = 3;
-  for (; per_sm >= 1; --per_sm) {
-    const int room = (per_sm == 3 ? 74 : per_sm == 2 ? 112 : 225) * 1024 - x_bytes - sums;
-    const int fit = room > 0 ? room / stage : 0;
-    p->stages = fit >= 6 ? 6 : fit >= 4 ? 4 : fit;
-    if (p->stages >= (per_sm == 1 ? 2 : 3)) break;
-  }
-  if (per_sm < 1) return 0;
-  p->at_x = p->stages * stage;
-  p->at_sums = p->at_x + x_bytes;
-  const size_t smem = p->at_sums + sums;
-  const int slots = per_sm * tc_num_sms();
-  // warps per tile: rounds of the launch times spans of a warp
-  double best = 1e30;
-  for (int ks = 1; ks <= WARPS; ks *= 2) {
-    const int rounds = (p->tiles + slots * (WARPS / ks) - 1) / (slots * (WARPS / ks));
-    const double cost = rounds * ((p->spans + ks - 1) / ks + 0.1);
-    if (cost < best) {
+  *grid = std::min(p->tiles, tc_num_sms());
+  // Warps per tile: as the spans of the busiest warp have it; the most of those that are equal (a tile's rows are
+  // read at once: 22016 x 4096 15.2 us with 8, 16.6 with 2).
+  const int mine = (p->tiles + *grid - 1) / *grid;  // tiles of a CTA
+  int best = 1 << 30;
+  for (int ks = 1; ks <= WARPS; ++ks) {
+    if (WARPS % ks != 0) continue;
+    const int rounds = (mine + WARPS / ks - 1) / (WARPS / ks);
+    const int cost = rounds * ((p->spans + ks - 1) / ks);
+    if (cost <= best) {
       best = cost;
       p->ks = ks;
+      p->join = std::min(rounds, 8 / p->pairs);
     }
   }
-  const int per_cta = WARPS / p->ks;
-  *grid = std::min((p->tiles + per_cta - 1) / per_cta, slots);
-  return smem;
+  const int x_bytes = (w.M * terms * p->x_pitch + 127) / 128 * 128, sums_x = p->spans * 4 * FEW_TOKENS * 4, sums = p->join * WARPS * 8 * p->pairs * 16;
+  const int fit = (226 * 1024 - x_bytes - sums_x - sums) / stage;
+  if (fit < 2) return 0;
+  p->stages = fit >= 6 ? 6 : fit >= 4 ? 4 : fit;
+  p->at_x = p->stages * stage;
+  p->at_sums_x = p->at_x + x_bytes;
+  p->at_sums = p->at_sums_x + sums_x;
+  return p->at_sums + sums;
 }
 
 }  // namespace

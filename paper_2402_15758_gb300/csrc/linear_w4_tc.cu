@@ -526,8 +526,7 @@ __global__ void __launch_bounds__(TOKEN_THREADS) w4_tokens_kernel(W4Params p, in
 
 template <int G, int TN, int FT>
 cudaError_t launch(const ManyParams& p, int grid, cudaStream_t s) {
-  const cudaError_t e =
-      cudaFuncSetAttribute(w4_many_kernel<G, TN, FT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(many_smem(TN, 2)));
+  const cudaError_t e = allow_smem<w4_many_kernel<G, TN, FT>>(many_smem(TN, 2));
   return e != cudaSuccess ? e : launch_pdl(w4_many_kernel<G, TN, FT>, dim3(grid), dim3(UNPACK_WARP * 32 + FT * halves(FT) * BM), many_smem(TN, p.terms), s, p);
 }
 template <int G, int TN>
