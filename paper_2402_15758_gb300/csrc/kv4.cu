@@ -1,5 +1,7 @@
 // The 4-bit KV cache's rows: written from fresh K and V rows, read back, and moved when the rows
 // that drew little attention leave (layout and rounding rule in kv4.cuh).
+#include <algorithm>
+
 #include "kernels.h"
 #include "kv4.cuh"
 #include "launch.cuh"
@@ -34,26 +36,6 @@ struct RowArgs {
 
 // Eight consecutive values of a row.
 template <typename T>
-__device__ __forceinline__ void load8(const T* src, bool vec, float (&x)[8]) {
-  if (!vec) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = to_f<T>(src[j]);
-    return;
-  }
-  if constexpr (sizeof(T) == 4) {
-    *reinterpret_cast<float4*>(x) = reinterpret_cast<const float4*>(src)[0];
-    *reinterpret_cast<float4*>(x + 4) = reinterpret_cast<const float4*>(src)[1];
-  } else {
-    const uint4 u = *reinterpret_cast<const uint4*>(src);
-    const uint32_t h[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(h[i] << 16);
-      x[2 * i + 1] = __uint_as_float(h[i] & 0xffff0000u);
-    }
-  }
-}
-template <typename T>
 __device__ __forceinline__ void store8(T* dst, bool vec, const float (&x)[8]) {
   if (!vec) {
 #pragma unroll
@@ -79,105 +61,148 @@ __device__ __forceinline__ void store8(T* dst, bool vec, const float (&x)[8]) {
 template <int HD>
 struct Piece {
   static constexpr int LANES = HD / 8;  // threads of a row
-  bool any, there[2];
+  bool there[2];
   int which, slot, part, g;  // slot: of the pair's first row; part: which eight channels
   long long row[2];          // of k and v
-  unsigned char* page;
-  __device__ __forceinline__ Piece(const RowArgs& a, const Kv4Pool& c, int pairs) {
-    const long long id = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x;
-    part = static_cast<int>(id % LANES);
-    long long i = id / LANES;
-    any = i < 2LL * c.B * pairs * c.G;
-    if (!any) i = 0;
-    g = static_cast<int>(i % c.G);
-    i /= c.G;
-    which = static_cast<int>(i & 1);
-    const int at = static_cast<int>((i >> 1) % pairs), b = static_cast<int>((i >> 1) / pairs);
+  // Block: heads (K's, then V's) by pairs; grid: pairs, heads, sequences.  Nothing is divided.
+  __device__ __forceinline__ Piece(const RowArgs& a, const Kv4Pool& c, int pairs, int at) {
+    const int piece = blockIdx.y * blockDim.x + threadIdx.x, of_k = c.G * LANES, b = blockIdx.z;
+    const bool any = piece < 2 * of_k && at < pairs;
+    which = piece >= of_k;
+    part = piece % LANES;
+    g = any ? (which ? piece - of_k : piece) / LANES : 0;
     const int s0 = a.slot0[b], count = a.counts ? min(a.counts[b], a.rows) : a.rows;
     slot = (s0 & ~1) + 2 * at;
-    page = nullptr;
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
       const int k = slot + r - s0;
       there[r] = any && k >= 0 && k < count;
       row[r] = static_cast<long long>(b) * a.rows + max(k, 0);
     }
-    if (there[0] || there[1]) page = page_of(c, b, g, slot);
-    if (!page) any = there[0] = there[1] = false;
+  }
+  __device__ __forceinline__ unsigned char* page(const RowArgs& a) const {
+    return there[0] || there[1] ? page_of(a.c, blockIdx.z, g, slot) : nullptr;
   }
 };
 
 // Rounds a row's eight values of this thread: the row's minimum and maximum over its LANES threads, then the codes,
-// four bits each.  A code is rint of the correctly rounded quotient; the product with the reciprocal
-// decides it alone unless it lies within 2^-16 of a tie.
+// four bits each.  A code is rint of the correctly rounded quotient, which one step of Markstein's correction
+// (q + (d - q step) / step, the remainder in one rounding) gives here: a step has 8 bits, so the remainder is
+// exact, and no quotient of 24 bits by 8 lies within 2^-10 units of a point where its rounding turns.  (bf16 values
+// meet ties too often for a branch around a division: 41 us for 4 x 1000 rows of 32 heads.)
+__device__ __forceinline__ float reciprocal(float x) {  // to 2^-23, for normal numbers: the correction needs no more
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+constexpr float ROUNDER = 12582912.f;  // 3 2^22: a sum with it is rounded to a whole number, in its last bits
+constexpr uint32_t ROUNDER_BITS = 0x4b400000u;
 template <int LANES>
 __device__ __forceinline__ uint32_t round8(const float (&x)[8], uint32_t& scale) {
-  float lo = x[0], hi = x[0];
-  bool fine = true;
+  float lo = x[0], hi = x[0], bad = 0.f;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     lo = fminf(lo, x[j]);
     hi = fmaxf(hi, x[j]);
-    fine = fine && isfinite(x[j]);
+    bad = fmaf(x[j], 0.f, bad);  // NaN from a value that is not finite
   }
 #pragma unroll
   for (int o = LANES / 2; o; o >>= 1) {
     lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
     hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    fine = __shfl_xor_sync(0xffffffffu, fine, o) && fine;
   }
+  const uint32_t spoilt = __ballot_sync(0xffffffffu, bad != 0.f) >> (threadIdx.y * blockDim.x + threadIdx.x) % 32 / LANES * LANES;
   const bf16 base16 = __float2bfloat16_rn(lo), step16 = __float2bfloat16_rn(__fmul_rn(hi - lo, 1.f / 15.f));
   const float base = __bfloat162float(base16), step = __bfloat162float(step16);
-  fine = fine && isfinite(hi - lo) && isfinite(base);
+  const bool fine = (spoilt & ((1u << LANES) - 1u)) == 0 && isfinite(hi - lo) && isfinite(base);
   scale = fine ? __bfloat16_as_ushort(step16) | static_cast<uint32_t>(__bfloat16_as_ushort(base16)) << 16 : 0x7fc00000u;
   if (!fine || !(step > 0.f)) return 0;
-  const float inv = 1.f / step;
+  // (a power of two keeps the reciprocal and the remainder among the normal numbers)
+  const float up = step < 0x1p-60f ? 0x1p100f : step > 0x1p60f ? 0x1p-100f : 1.f, unit = step * up, inv = reciprocal(unit);
   uint32_t codes = 0;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float d = x[j] - base;
-    float q = d * inv, n = rintf(q);
-    if (!(fabsf(q - n) < 0.5f - 0x1p-16f)) n = rintf(__fdiv_rn(d, step));
-    codes |= static_cast<uint32_t>(fminf(fmaxf(n, 0.f), 15.f)) << (4 * j);
+  for (int j = 7; j >= 0; --j) {
+    const float d = (x[j] - base) * up, q = d * inv;
+    const float exact = fmaf(fmaf(-q, unit, d), inv, q);
+    codes = codes * 16 + (__float_as_uint(fminf(fmaxf(exact, 0.f), 15.f) + ROUNDER) - ROUNDER_BITS);
   }
   return codes;
 }
+
+// Eight values as they lie, converted when they are used.
+template <typename T>
+struct Raw {
+  uint32_t u[2 * sizeof(T)];
+  __device__ __forceinline__ void load(const T* src, bool vec) {
+    if (vec) {
+#pragma unroll
+      for (int i = 0; i < sizeof(T) / 2; ++i) *reinterpret_cast<uint4*>(u + 4 * i) = reinterpret_cast<const uint4*>(src)[i];
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(src[j]);
+    } else {
+      const uint16_t* h = reinterpret_cast<const uint16_t*>(src);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) u[i] = h[2 * i] | static_cast<uint32_t>(h[2 * i + 1]) << 16;
+    }
+  }
+  __device__ __forceinline__ void values(float (&x)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      x[j] = __uint_as_float(sizeof(T) == 4 ? u[j % (2 * sizeof(T))] : j & 1 ? u[j / 2] & 0xffff0000u : u[j / 2] << 16);
+  }
+};
+
+constexpr int APPEND_PAIRS = 2;  // of a thread, all their loads in flight
 
 template <int HD, typename T>
 __global__ void __launch_bounds__(256) kv4_append_kernel(RowArgs a, int pairs) {
   pdl_wait();
   pdl_trigger();
   using P = Kv4<HD>;
-  const Piece<HD> w(a, a.c, pairs);
-  float x[2][8];
-  uint32_t codes[2], scale[2];
+  const int first = blockIdx.x * blockDim.y * APPEND_PAIRS;
+  Raw<T> raw[APPEND_PAIRS][2];
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
+  for (int i = 0; i < APPEND_PAIRS; ++i) {
+    const Piece<HD> w(a, a.c, pairs, first + i * blockDim.y + threadIdx.y);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[r][j] = 0.f;
-    if (w.there[r])
-      load8<T>(static_cast<const T*>(w.which ? a.v : a.k) + w.row[r] * (w.which ? a.ldv : a.ldk) + w.g * HD + 8 * w.part, a.vec, x[r]);
-  }
-#pragma unroll
-  for (int r = 0; r < 2; ++r) codes[r] = round8<Piece<HD>::LANES>(x[r], scale[r]);
-  if (!w.any) return;
-  const int row = w.slot % KV4_ROWS;
-  if (!w.which) {
-#pragma unroll
-    for (int r = 0; r < 2; ++r)
-      if (w.there[r]) *reinterpret_cast<uint32_t*>(w.page + (row + r) * P::ROW + 4 * w.part) = codes[r];
-  } else {
-    unsigned char* at = w.page + P::v_half(row, 2 * w.part);  // words 2 part and 2 part + 1 are neighbours
-    if (w.there[0] && w.there[1]) {
-      *reinterpret_cast<uint2*>(at) = make_uint2(__byte_perm(codes[0], codes[1], 0x5410), __byte_perm(codes[0], codes[1], 0x7632));
-    } else {
-      const int r = w.there[0] ? 0 : 1;
-      *reinterpret_cast<uint16_t*>(at + 2 * r) = static_cast<uint16_t>(codes[r]);
-      *reinterpret_cast<uint16_t*>(at + 2 * r + 4) = static_cast<uint16_t>(codes[r] >> 16);
+    for (int r = 0; r < 2; ++r) {
+      raw[i][r] = Raw<T>{};
+      if (w.there[r])
+        raw[i][r].load(static_cast<const T*>(w.which ? a.v : a.k) + w.row[r] * (w.which ? a.ldv : a.ldk) + w.g * HD + 8 * w.part, a.vec);
     }
   }
-  if (w.part < 2 && w.there[w.part])
-    *reinterpret_cast<uint32_t*>(w.page + (w.which ? P::VS : P::KS) + 4 * (row + w.part)) = w.part ? scale[1] : scale[0];
+#pragma unroll
+  for (int i = 0; i < APPEND_PAIRS; ++i) {
+    if (first + i * static_cast<int>(blockDim.y) >= pairs) return;  // (the whole block)
+    const Piece<HD> w(a, a.c, pairs, first + i * blockDim.y + threadIdx.y);
+    unsigned char* page = w.page(a);
+    uint32_t codes[2], scale[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      float x[8];
+      raw[i][r].values(x);
+      codes[r] = round8<Piece<HD>::LANES>(x, scale[r]);
+    }
+    if (!page) continue;
+    const int row = w.slot % KV4_ROWS;
+    if (!w.which) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+        if (w.there[r]) *reinterpret_cast<uint32_t*>(page + (row + r) * P::ROW + 4 * w.part) = codes[r];
+    } else {
+      unsigned char* at = page + P::v_half(row, 2 * w.part);  // words 2 part and 2 part + 1 are neighbours
+      if (w.there[0] && w.there[1]) {
+        *reinterpret_cast<uint2*>(at) = make_uint2(__byte_perm(codes[0], codes[1], 0x5410), __byte_perm(codes[0], codes[1], 0x7632));
+      } else {
+        const int r = w.there[0] ? 0 : 1;
+        *reinterpret_cast<uint16_t*>(at + 2 * r) = static_cast<uint16_t>(codes[r]);
+        *reinterpret_cast<uint16_t*>(at + 2 * r + 4) = static_cast<uint16_t>(codes[r] >> 16);
+      }
+    }
+    if (w.part < 2 && (w.part ? w.there[1] : w.there[0]))
+      *reinterpret_cast<uint32_t*>(page + (w.which ? P::VS : P::KS) + 4 * (row + w.part)) = w.part ? scale[1] : scale[0];
+  }
 }
 
 template <int HD, typename T>
@@ -185,25 +210,27 @@ __global__ void __launch_bounds__(256) kv4_read_kernel(RowArgs a, int pairs) {
   pdl_wait();
   pdl_trigger();
   using P = Kv4<HD>;
-  const Piece<HD> w(a, a.c, pairs);
-  if (!w.any) return;
+  const Piece<HD> w(a, a.c, pairs, blockIdx.x * blockDim.y + threadIdx.y);
+  const unsigned char* page = w.page(a);
+  if (!page) return;
   const int row = w.slot % KV4_ROWS;
   uint2 c;  // codes of the pair's rows
   if (!w.which) {
-    c.x = *reinterpret_cast<const uint32_t*>(w.page + row * P::ROW + 4 * w.part);
-    c.y = *reinterpret_cast<const uint32_t*>(w.page + (row + 1) * P::ROW + 4 * w.part);
+    c.x = *reinterpret_cast<const uint32_t*>(page + row * P::ROW + 4 * w.part);
+    c.y = *reinterpret_cast<const uint32_t*>(page + (row + 1) * P::ROW + 4 * w.part);
   } else {
-    c = *reinterpret_cast<const uint2*>(w.page + P::v_half(row, 2 * w.part));
+    c = *reinterpret_cast<const uint2*>(page + P::v_half(row, 2 * w.part));
     c = make_uint2(__byte_perm(c.x, c.y, 0x5410), __byte_perm(c.x, c.y, 0x7632));
   }
-  const uint2 scale = *reinterpret_cast<const uint2*>(w.page + (w.which ? P::VS : P::KS) + 4 * row);
+  const uint2 scale = *reinterpret_cast<const uint2*>(page + (w.which ? P::VS : P::KS) + 4 * row);
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
     if (!w.there[r]) continue;
     const uint32_t codes = r ? c.y : c.x, s = r ? scale.y : scale.x;
     float x[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = fmaf(kv4_step(s), static_cast<float>(codes >> (4 * j) & 15u), kv4_base(s));
+    for (int j = 0; j < 8; ++j)  // (a code as the last bits of 2^23: a conversion takes four times as long)
+      x[j] = fmaf(kv4_step(s), __uint_as_float(and_or(codes >> (4 * j), 15u, 0x4b000000u)) - 8388608.f, kv4_base(s));
     store8<T>(static_cast<T*>(w.which ? a.v : a.k) + w.row[r] * (w.which ? a.ldv : a.ldk) + w.g * HD + 8 * w.part, a.vec, x);
   }
 }
@@ -413,10 +440,13 @@ __global__ void __launch_bounds__(128 * MOVE_PAGES) kv4_move_kernel(Kv4EvictPara
 
 // The rows of a call lie in rows / 2 + 1 pairs of slots at most, wherever the first one starts.
 template <typename K>
-cudaError_t launch_rows(K kernel, const RowArgs& a, cudaStream_t s) {
-  const int pairs = a.rows / 2 + 1;
-  const long long threads = 2LL * a.c.B * pairs * a.c.G * (a.c.hd / 8);
-  return launch_pdl(kernel, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, s, a, pairs);
+cudaError_t launch_rows(K kernel, const RowArgs& a, cudaStream_t s, int each = 1) {  // each: pairs of a thread
+  const int pairs = a.rows / 2 + 1, pieces = 2 * a.c.G * (a.c.hd / 8);
+  int x = std::min(pieces, 256);
+  if (x > 128 && x % 32) x = 128;
+  int y = 256 / x;
+  y -= x * y % 32 ? y % 2 : 0;  // whole warps (pieces are a multiple of 16)
+  return launch_pdl(kernel, dim3((pairs + y * each - 1) / (y * each), (pieces + x - 1) / x, a.c.B), dim3(x, y), 0, s, a, pairs);
 }
 RowArgs row_args(const Kv4Pool& c, void* k, void* v, int f32, int ldk, int ldv, int rows, const int* slot0, const int* counts) {
   const int wide = f32 ? 4 : 8;  // values in 16 bytes
@@ -430,8 +460,8 @@ cudaError_t kv4_append(const Kv4Pool& c, const void* k, const void* v, int f32, 
                        const int* slot0, const int* counts, cudaStream_t s) {
   const RowArgs a = row_args(c, const_cast<void*>(k), const_cast<void*>(v), f32, ldk, ldv, rows, slot0, counts);
   if (c.hd == 128)
-    return f32 ? launch_rows(kv4_append_kernel<128, float>, a, s) : launch_rows(kv4_append_kernel<128, bf16>, a, s);
-  return f32 ? launch_rows(kv4_append_kernel<64, float>, a, s) : launch_rows(kv4_append_kernel<64, bf16>, a, s);
+    return f32 ? launch_rows(kv4_append_kernel<128, float>, a, s, APPEND_PAIRS) : launch_rows(kv4_append_kernel<128, bf16>, a, s, APPEND_PAIRS);
+  return f32 ? launch_rows(kv4_append_kernel<64, float>, a, s, APPEND_PAIRS) : launch_rows(kv4_append_kernel<64, bf16>, a, s, APPEND_PAIRS);
 }
 
 cudaError_t kv4_read(const Kv4Pool& c, void* k, void* v, int f32, int ldk, int ldv, int rows, const int* slot0,
