@@ -774,7 +774,6 @@ __global__ void __launch_bounds__(WARPS * 32) score_kv4_kernel(const __grid_cons
       float step[4], base[4], sum[4] = {};
       key_scales(page + P::V, t, step, base);
       const int slot0 = (p0 + warp + k * WARPS) * KV4_ROWS;
-      const bool whole = slot0 + KV4_ROWS <= all.n;
       // the page's codes, unpacked once for all tiles
       constexpr int NW = HD / 32;
       uint32_t codes[2][NW][4];
@@ -791,8 +790,7 @@ __global__ void __launch_bounds__(WARPS * 32) score_kv4_kernel(const __grid_cons
           for (int w = 0; w < NW; ++w) kv4_codes(k[h][w], codes[h][w]);
         }
       }
-#pragma unroll 2
-      for (int i = 0; i < held; ++i) {
+      auto tile = [&](int i, auto hidden) {  // hidden(row of the tile, j): is key j hidden from it?
         float s[2][4];
 #pragma unroll
         for (int j = 0; j < HD / 16; ++j) {
@@ -806,21 +804,35 @@ __global__ void __launch_bounds__(WARPS * 32) score_kv4_kernel(const __grid_cons
           }
         }
         const float4 rf = reinterpret_cast<const float4*>(smem + S::ROWF)[i * ROWS + r];
-        Seen seen = all;
-        if (!whole) seen.local = reinterpret_cast<const unsigned long long*>(smem + S::LOCAL)[i * ROWS + r];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           const float z = fmaf(step[x] * rf.x, s[x / 2][x % 2] + s[x / 2][2 + x % 2], base[x] * rf.y);
-          if (rf.w != 0.f && (whole || seen(slot0 + 2 * t + (x & 1) + 8 * (x >> 1)))) sum[x] = fmaf(rf.w, pow2(z - rf.z), sum[x]);
+          const float e = rf.w * pow2(z - rf.z);
+          sum[x] += hidden(i * ROWS + r, x) ? 0.f : e;
         }
+      };
+      if (slot0 + KV4_ROWS <= all.n) {
+        // every row sees these keys; rows past the last have weight 0 and logits of 0
+#pragma unroll 2
+        for (int i = 0; i < held; ++i) tile(i, [](int, int) { return false; });
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < held; ++i)
+          tile(i, [&](int row, int x) {
+            Seen seen = all;
+            seen.local = reinterpret_cast<const unsigned long long*>(smem + S::LOCAL)[row];
+            return !(seen(slot0 + 2 * t + (x & 1) + 8 * (x >> 1)) && reinterpret_cast<const float4*>(smem + S::ROWF)[row].w != 0.f);
+          });
       }
+      // over the rows: a lane hands on half of its sums at each step, and lanes r = 2 x, 2 x + 1 end with that of key x
+      float half[2], whole;
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-#pragma unroll
-        for (int s = 4; s < 32; s <<= 1) sum[x] += __shfl_xor_sync(0xffffffffu, sum[x], s);
-        const int slot = slot0 + 2 * t + (x & 1) + 8 * (x >> 1);
-        if (r == x && slot < all.total && slot < p.ld_scores) scores[slot] += sum[x];
-      }
+      for (int x = 0; x < 2; ++x) half[x] = (r & 4 ? sum[2 + x] : sum[x]) + __shfl_xor_sync(0xffffffffu, r & 4 ? sum[x] : sum[2 + x], 16);
+      whole = (r & 2 ? half[1] : half[0]) + __shfl_xor_sync(0xffffffffu, r & 2 ? half[0] : half[1], 8);
+      whole += __shfl_xor_sync(0xffffffffu, whole, 4);
+      const int slot = slot0 + 2 * t + (r >> 1 & 1) + 8 * (r >> 2);
+      // (its only writer: a sum in memory, so that the warp waits for no old value)
+      if (!(r & 1) && slot < all.total && slot < p.ld_scores) red_add_f32(scores + slot, whole);
       __syncwarp();
       if (k + STAGES < mine) request(k + STAGES);
     }
