@@ -95,6 +95,15 @@ __device__ __forceinline__ void tmem_wait_cols(uint32_t (&r)[N]) {
     asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]));
 }
 
+// a += s x, b += s y in one instruction.
+__device__ __forceinline__ void fma2(float s, float x, float y, float& a, float& b) {
+  asm("{\n\t.reg .b64 s, v, t;\n\t"
+      "mov.b64 s, {%2, %2};\n\tmov.b64 v, {%3, %4};\n\tmov.b64 t, {%0, %1};\n\t"
+      "fma.rn.f32x2 t, s, v, t;\n\tmov.b64 {%0, %1}, t;\n\t}"
+      : "+f"(a), "+f"(b)
+      : "f"(s), "f"(x), "f"(y));
+}
+
 __device__ __forceinline__ int cta_of_unit(uint32_t u, uint32_t U, uint32_t G) { return static_cast<int>(((u + 1) * G - 1) / U); }
 __device__ __forceinline__ uint32_t unit_begin(uint32_t c, uint32_t U, uint32_t G) { return c * U / G; }
 
@@ -321,7 +330,7 @@ __global__ void __launch_bounds__(UNPACK_WARP * 32 + FT * halves(FT) * BM, 1) w4
       const float s = summed & 1 ? scale_of[1] : scale_of[0];
       tmem_wait_cols<ONCE>(d);
 #pragma unroll
-      for (int j = 0; j < ONCE; ++j) acc[at + j] = fmaf(s, __uint_as_float(d[j]), acc[at + j]);
+      for (int j = 0; j < ONCE; j += 2) fma2(s, __uint_as_float(d[j]), __uint_as_float(d[j + 1]), acc[at + j], acc[at + j + 1]);
     };
     // Slot 0 of a CTA holds its first tile's part, slot 1 its last one's.
     auto slot_of = [&](int c, int t) { return 2 * c + (unit_begin(c, U, CTAS) / KS == static_cast<uint32_t>(t) ? 0 : 1); };
