@@ -384,7 +384,8 @@ struct Kv4AttnParams {
   bf16_raw* out_lo;   // optional (bf16 out)
   int out_f32, ldo;
   float* lse;         // optional [B * q_rows][H]; the score kernel's input
-  int splits;
+  int splits;         // of every sequence; or, with slots, those of the grid that are dealt to the sequences by
+  int slots, least_pages;  // their lengths, parts of at least so many pages
   float* ws;
   // score: scores[(b * G + g) * ld_scores + slot] += sum over the rows of weight p
   float* scores;
@@ -392,8 +393,7 @@ struct Kv4AttnParams {
   const float* weight;  // optional [B * q_rows]
 };
 int kv4_attn_blocks(const Kv4AttnParams& p);  // of the grid, without its splits
-int kv4_attn_splits(const Kv4AttnParams& p);
-size_t kv4_attn_ws_floats(const Kv4AttnParams& p);
+void kv4_attn_split(Kv4AttnParams* p, int want, size_t most_floats);
 cudaError_t attention_kv4(const Kv4AttnParams& p, cudaStream_t s);
 cudaError_t kv4_score(const Kv4AttnParams& p, cudaStream_t s);
 

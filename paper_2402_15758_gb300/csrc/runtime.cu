@@ -2233,9 +2233,8 @@ chimera_status chimera_op_attention_kv4(int q_dtype, int out_dtype, int batch, i
   p.out_f32 = out_dtype == 0;
   p.ldo = ldo;
   p.lse = lse;
-  p.splits = splits ? splits : kv4_attn_splits(p);
   if (kv4_attn_blocks(p) > 65535) return CHIMERA_EINVAL;
-  while (p.splits > 1 && kv4_attn_ws_floats(p) > OP_ATT_FLOATS) --p.splits;
+  kv4_attn_split(&p, splits, OP_ATT_FLOATS);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   std::lock_guard<std::mutex> lk(g_op_mu);
   OpScratch* sc = op_scratch(s);

@@ -324,6 +324,24 @@ def test_attention_kv4(case, splits, form):
         assert float((got - lse_ref)[~empty].abs().max() if (~empty).any() else 0) <= ATT_TOL * 10  # of logits up to about 20
 
 
+# batches whose pages are dealt by their lengths: fewer slots of the grid than every sequence could use
+RAGGED = [
+    ([2049, 0, 130, 900, 1], 32, 32, 64, 1, 0, 1, "chain"),
+    ([1900, 0, 17], 40, 40, 128, 2, 0, 0, "none"),        # a sequence that sees nothing
+    ([700, 3, 1500, 64], 16, 16, 128, 40, 0, 40, "tree"),
+    ([40 * i for i in range(32)], 8, 16, 128, 2, 0, 2, "chain"),
+    ([1500] + [0] * 30 + [9], 16, 16, 64, 1, 0, 1, "chain"),
+    ([30 * i for i in range(33)], 8, 8, 64, 1, 0, 1, "chain"),  # more sequences than are dealt
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", RAGGED)
+@pytest.mark.parametrize("form", ["f32", "pair", "bf16"])
+def test_attention_kv4_ragged(case, form):
+    test_attention_kv4(case, 0, form)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("size", [1e-12, 1e-3, 1e6])
 def test_attention_kv4_any_size_of_values(size):
