@@ -178,6 +178,14 @@ __device__ __forceinline__ Deal deal_slots(const Kv4AttnParams& p, int lane) {
   return d;
 }
 
+// The sequence of a slot of the grid, which becomes its part of the sequence's `splits`.
+__device__ __forceinline__ int sequence_of(const Deal& d, int& slot, int& splits) {
+  const int b = __popc(__ballot_sync(0xffffffffu, d.parts > 0 && d.first <= slot)) - 1;
+  slot -= __shfl_sync(0xffffffffu, d.first, b);
+  splits = __shfl_sync(0xffffffffu, d.parts, b);
+  return b;
+}
+
 // Block of the pool for page `at` of the sequence (block 0, with the error flagged, when the
 // table names none).
 __device__ __forceinline__ int block_of(const Kv4AttnParams& p, const int* table, int at) {
@@ -261,9 +269,7 @@ __global__ void __launch_bounds__(WARPS * 32, NM == 1 ? 3 : 2) attn_kv4_kernel(c
   int b = bg0 / p.c.G, split = blockIdx.x, splits = gridDim.x;
   if (DEAL) {
     const Deal d = deal_slots(p, lane);
-    b = __popc(__ballot_sync(0xffffffffu, d.parts > 0 && d.first <= split)) - 1;
-    split -= __shfl_sync(0xffffffffu, d.first, b);
-    splits = __shfl_sync(0xffffffffu, d.parts, b);
+    b = sequence_of(d, split, splits);
     if (split >= splits) return;  // (the whole block; a slot that is left over)
   }
   const int bg = b * p.c.G + g;
@@ -728,7 +734,7 @@ struct ScoreSmem {
   static constexpr int BYTES = LOCAL + SCORE_TILES * ROWS * 8;
 };
 
-template <int HD, typename TQ>
+template <int HD, typename TQ, bool DEAL>
 __global__ void __launch_bounds__(WARPS * 32) score_kv4_kernel(const __grid_constant__ Kv4AttnParams p) {
   extern __shared__ __align__(128) unsigned char smem[];
   using S = ScoreSmem<HD>;
@@ -746,7 +752,14 @@ __global__ void __launch_bounds__(WARPS * 32) score_kv4_kernel(const __grid_cons
   pdl_wait();
   pdl_trigger();
 
-  const int group = p.H / p.c.G, bg = blockIdx.y, b = bg / p.c.G, g = bg % p.c.G;
+  const int group = p.H / p.c.G, g = blockIdx.y % p.c.G;
+  int b = blockIdx.y / p.c.G, split = blockIdx.x, splits = gridDim.x;
+  if (DEAL) {
+    const Deal d = deal_slots(p, lane);
+    b = sequence_of(d, split, splits);
+    if (split >= splits) return;  // (the whole block; a slot that is left over)
+  }
+  const int bg = b * p.c.G + g;
   // the queries that count
   if (warp == 0) {
     int found = 0;
@@ -763,7 +776,6 @@ __global__ void __launch_bounds__(WARPS * 32) score_kv4_kernel(const __grid_cons
   const Seen all = what_is_seen(p, b);
   const int pages = (min(all.total, p.ld_scores) + KV4_ROWS - 1) / KV4_ROWS;
   if (all.total > p.ld_scores && tid == 0) atomicOr(p.c.err, ERR_CAPACITY);
-  const int split = blockIdx.x, splits = gridDim.x;
   const int p0 = static_cast<int>(static_cast<long long>(pages) * split / splits);
   const int p1 = static_cast<int>(static_cast<long long>(pages) * (split + 1) / splits);
   const int mine = max(0, (p1 - p0 - warp + WARPS - 1) / WARPS);
@@ -977,15 +989,23 @@ cudaError_t attention_kv4(const Kv4AttnParams& p, cudaStream_t s) {
   return p.q_f32 ? launch_cut<64, float>(p, s) : launch_cut<64, bf16>(p, s);
 }
 
-cudaError_t kv4_score(const Kv4AttnParams& p, cudaStream_t s) {
-  const int bg = p.c.B * p.c.G;
-  const int most = (p.c.max_pages + WARPS - 1) / WARPS;
-  const dim3 grid(std::max(1, std::min(4 * tc_num_sms() / bg, most)), bg);  // four blocks per SM
-  if (p.c.hd == 128)
-    return p.q_f32 ? launch_sized<score_kv4_kernel<128, float>>(ScoreSmem<128>::BYTES, grid, p, s)
-                   : launch_sized<score_kv4_kernel<128, bf16>>(ScoreSmem<128>::BYTES, grid, p, s);
-  return p.q_f32 ? launch_sized<score_kv4_kernel<64, float>>(ScoreSmem<64>::BYTES, grid, p, s)
-                 : launch_sized<score_kv4_kernel<64, bf16>>(ScoreSmem<64>::BYTES, grid, p, s);
+namespace {
+template <int HD, typename TQ>
+cudaError_t launch_score(const Kv4AttnParams& p, const dim3& grid, cudaStream_t s) {
+  return p.slots ? launch_sized<score_kv4_kernel<HD, TQ, true>>(ScoreSmem<HD>::BYTES, grid, p, s)
+                 : launch_sized<score_kv4_kernel<HD, TQ, false>>(ScoreSmem<HD>::BYTES, grid, p, s);
+}
+}  // namespace
+
+cudaError_t kv4_score(const Kv4AttnParams& call, cudaStream_t s) {
+  Kv4AttnParams p = call;
+  const int bg = p.c.B * p.c.G, resident = 4 * tc_num_sms();  // four blocks per SM
+  const int most = (p.c.max_pages + WARPS - 1) / WARPS, slots = resident / p.c.G;
+  p.least_pages = WARPS;
+  p.slots = p.c.B > 1 && p.c.B <= DEAL_MOST && slots > p.c.B && slots < p.c.B * std::min(most, PARTS_MOST) ? slots : 0;
+  const dim3 grid = p.slots ? dim3(p.slots, p.c.G) : dim3(std::max(1, std::min(resident / bg, most)), bg);
+  if (p.c.hd == 128) return p.q_f32 ? launch_score<128, float>(p, grid, s) : launch_score<128, bf16>(p, grid, s);
+  return p.q_f32 ? launch_score<64, float>(p, grid, s) : launch_score<64, bf16>(p, grid, s);
 }
 
 }  // namespace chimera

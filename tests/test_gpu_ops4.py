@@ -396,6 +396,12 @@ def test_score_kv4(case, weighted):
         assert torch.equal(scores[b, :, ctx[b] + n_local:].double(), want[b, :, ctx[b] + n_local:])
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", RAGGED)
+def test_score_kv4_ragged(case):
+    test_score_kv4(case, True)
+
+
 # ---------------------------------------------------------------------------------------
 # eviction
 # ---------------------------------------------------------------------------------------
