@@ -1,6 +1,7 @@
 // The 4-bit KV cache's rows: written from fresh K and V rows, read back, and moved when the rows
 // that drew little attention leave (layout and rounding rule in kv4.cuh).
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
 #include "kv4.cuh"
@@ -369,72 +370,79 @@ __global__ void __launch_bounds__(SEL_THREADS) kv4_select_kernel(Kv4EvictParams 
   });
 }
 
-// 128 threads per (destination page, sequence and head) gather the 16 rows kept there, 16 bytes a time: a K row's codes
-// as they are, a V chunk from the chunks of its two rows.  Four pages per block.
-constexpr int MOVE_PAGES = 4;
+// 128 threads gather the 16 rows kept in a destination page, 16 bytes a time: a K row's codes as they are, a V chunk from
+// the chunks of its two rows.  A block finds the rows of 8 pages at once, and a thread has its loads of two pages in
+// flight: 2 x 8192 rows of 32 heads (142 MB; 205 MB with the sectors that hold them) 34 us, 6 TB/s of sectors.  One
+// page a thread took 46 us, waiting for slot, table entry and codes in turn, four pages (58 registers) 44.
+constexpr int MOVE_ONCE = 2, MOVE_PAGES = 4 * MOVE_ONCE;
 template <int HD>
-__global__ void __launch_bounds__(128 * MOVE_PAGES) kv4_move_kernel(Kv4EvictParams p) {
+__global__ void __launch_bounds__(512, 4) kv4_move_kernel(Kv4EvictParams p) {
   pdl_wait();
   pdl_trigger();
   using P = Kv4<HD>;
   const int bg = blockIdx.y, b = bg / p.c.G, g = bg % p.c.G, tid = threadIdx.x % 128, which = threadIdx.x / 128;
-  const int page = blockIdx.x * MOVE_PAGES + which;
-  __shared__ const unsigned char* sh_src[MOVE_PAGES][KV4_ROWS];
+  const int page0 = blockIdx.x * MOVE_PAGES;
+  __shared__ const unsigned char* sh_src[MOVE_PAGES][KV4_ROWS];  // pages of the rows, null from the first that is not kept
   __shared__ int sh_row[MOVE_PAGES][KV4_ROWS];
   __shared__ unsigned char* sh_dst[MOVE_PAGES];
-  const bool used = page * KV4_ROWS < p.budget;
-  if (tid < KV4_ROWS) {
-    const int i = page * KV4_ROWS + tid;
+  if (threadIdx.x < MOVE_PAGES * KV4_ROWS) {
+    const int i = page0 * KV4_ROWS + threadIdx.x;
     const int slot = i < p.budget ? p.kept[static_cast<size_t>(bg) * p.budget + i] : -1;
-    sh_src[which][tid] = slot >= 0 ? page_of(p.c, b, g, slot) : nullptr;
-    sh_row[which][tid] = slot & (KV4_ROWS - 1);
-  }
-  if (tid == KV4_ROWS) {
+    sh_src[threadIdx.x / KV4_ROWS][threadIdx.x % KV4_ROWS] = slot >= 0 ? page_of(p.c, b, g, slot) : nullptr;
+    sh_row[threadIdx.x / KV4_ROWS][threadIdx.x % KV4_ROWS] = slot & (KV4_ROWS - 1);
+  } else if (threadIdx.x < MOVE_PAGES * KV4_ROWS + MOVE_PAGES) {
+    const int at = threadIdx.x - MOVE_PAGES * KV4_ROWS;
     Kv4Pool d = p.c;
     d.table = p.dst_table;
     d.max_pages = p.dst_pages;
-    sh_dst[which] = used ? page_of(d, b, g, page * KV4_ROWS) : nullptr;
+    sh_dst[at] = (page0 + at) * KV4_ROWS < p.budget ? page_of(d, b, g, (page0 + at) * KV4_ROWS) : nullptr;
   }
   __syncthreads();
-  unsigned char* dst = sh_dst[which];
-  const unsigned char** src = sh_src[which];
-  const int* row_of = sh_row[which];
-  if (!dst || !src[0]) return;  // (the kept rows come first)
-  if (tid < 64) {
-    // V: pair tid / 8, chunk tid % 8
-    const int pair = tid / 8, chunk = tid % 8;
-    const unsigned char *s0 = src[2 * pair], *s1 = src[2 * pair + 1];
-    if (s0) {
-      const int r0 = row_of[2 * pair], r1 = s1 ? row_of[2 * pair + 1] : 0;
-      const unsigned char* a = s0 + P::V + r0 / 2 * 2 * P::ROW + P::place(r0 / 2, chunk) * P::CHUNK;
-      const unsigned char* c = s1 ? s1 + P::V + r1 / 2 * 2 * P::ROW + P::place(r1 / 2, chunk) * P::CHUNK : a;
-      unsigned char* to = dst + P::V + pair * 2 * P::ROW + P::place(pair, chunk) * P::CHUNK;
-      // halves of the words: row 2 pair from the half of its parity, row 2 pair + 1 likewise
-      const uint32_t pick = (r0 & 1 ? 0x32u : 0x10u) | (r1 & 1 ? 0x7600u : 0x5400u);
-      uint32_t x[P::CHUNK / 4], y[P::CHUNK / 4];
-      if constexpr (HD == 128) {
-        *reinterpret_cast<uint4*>(x) = *reinterpret_cast<const uint4*>(a);
-        *reinterpret_cast<uint4*>(y) = *reinterpret_cast<const uint4*>(c);
-      } else {
-        *reinterpret_cast<uint2*>(x) = *reinterpret_cast<const uint2*>(a);
-        *reinterpret_cast<uint2*>(y) = *reinterpret_cast<const uint2*>(c);
-      }
+  const bool is_v = tid < 64;
+  const int pair = tid / 8, chunk = tid % 8;                                             // V's
+  const int k_row = (tid - 64) / (P::ROW / 16), k_at = (tid - 64) % (P::ROW / 16) * 16;  // K's
+  const int first = is_v ? 2 * pair : k_row < KV4_ROWS ? k_row : -1;                      // row of the page
+  using Chunk = typename std::conditional<HD == 128, uint4, uint2>::type;
+  constexpr int WORDS = P::CHUNK / 4;
+  uint4 x[MOVE_ONCE];  // K: 16 bytes; V: the first row's chunk
+  Chunk y[MOVE_ONCE];  // V: the second row's
+  uint32_t scale[MOVE_ONCE];
 #pragma unroll
-      for (int i = 0; i < P::CHUNK / 4; ++i) x[i] = __byte_perm(x[i], y[i], pick);
-      if constexpr (HD == 128)
-        *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(x);
-      else
-        *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(x);
+  for (int j = 0; j < MOVE_ONCE; ++j) {
+    const int at = which * MOVE_ONCE + j;
+    if (!sh_dst[at]) continue;
+    const unsigned char* s0 = first >= 0 ? sh_src[at][first] : nullptr;
+    if (s0 && !is_v) x[j] = *reinterpret_cast<const uint4*>(s0 + sh_row[at][first] * P::ROW + k_at);
+    if (s0 && is_v) {
+      const int r0 = sh_row[at][first], r1 = sh_row[at][first + 1];
+      const unsigned char* s1 = sh_src[at][first + 1];
+      *reinterpret_cast<Chunk*>(x + j) = *reinterpret_cast<const Chunk*>(s0 + P::V + r0 / 2 * 2 * P::ROW + P::place(r0 / 2, chunk) * P::CHUNK);
+      y[j] = Chunk{};
+      if (s1) y[j] = *reinterpret_cast<const Chunk*>(s1 + P::V + r1 / 2 * 2 * P::ROW + P::place(r1 / 2, chunk) * P::CHUNK);
     }
     if (tid < 2 * KV4_ROWS) {
-      const int row = tid % KV4_ROWS, at = tid < KV4_ROWS ? P::KS : P::VS;
-      if (src[row])
-        *reinterpret_cast<uint32_t*>(dst + at + 4 * row) = *reinterpret_cast<const uint32_t*>(src[row] + at + 4 * row_of[row]);
+      const int row = tid % KV4_ROWS;
+      if (sh_src[at][row]) scale[j] = *reinterpret_cast<const uint32_t*>(sh_src[at][row] + (tid < KV4_ROWS ? P::KS : P::VS) + 4 * sh_row[at][row]);
     }
-  } else if (tid - 64 < KV4_ROWS * P::ROW / 16) {
-    const int row = (tid - 64) / (P::ROW / 16), c = (tid - 64) % (P::ROW / 16);
-    if (src[row])
-      *reinterpret_cast<uint4*>(dst + row * P::ROW + 16 * c) = *reinterpret_cast<const uint4*>(src[row] + row_of[row] * P::ROW + 16 * c);
+  }
+#pragma unroll
+  for (int j = 0; j < MOVE_ONCE; ++j) {
+    const int at = which * MOVE_ONCE + j;
+    unsigned char* dst = sh_dst[at];
+    if (!dst) continue;
+    const bool there = first >= 0 && sh_src[at][first];
+    if (there && !is_v) *reinterpret_cast<uint4*>(dst + k_row * P::ROW + k_at) = x[j];
+    if (there && is_v) {
+      // halves of the words: row 2 pair from the half of its parity, row 2 pair + 1 likewise
+      const uint32_t pick = (sh_row[at][first] & 1 ? 0x32u : 0x10u) | (sh_row[at][first + 1] & 1 ? 0x7600u : 0x5400u);
+      uint32_t* a = reinterpret_cast<uint32_t*>(x + j);
+      const uint32_t* c = reinterpret_cast<const uint32_t*>(y + j);
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) a[i] = __byte_perm(a[i], c[i], pick);
+      *reinterpret_cast<Chunk*>(dst + P::V + pair * 2 * P::ROW + P::place(pair, chunk) * P::CHUNK) = *reinterpret_cast<const Chunk*>(x + j);
+    }
+    if (tid < 2 * KV4_ROWS && sh_src[at][tid % KV4_ROWS])
+      *reinterpret_cast<uint32_t*>(dst + (tid < KV4_ROWS ? P::KS : P::VS) + 4 * (tid % KV4_ROWS)) = scale[j];
   }
 }
 
@@ -477,8 +485,8 @@ cudaError_t kv4_evict(const Kv4EvictParams& p, cudaStream_t s) {
   cudaError_t e = launch_pdl(kv4_select_kernel, dim3(bg), dim3(SEL_THREADS), 0, s, p);
   if (e != cudaSuccess) return e;
   const dim3 grid(((p.budget + KV4_ROWS - 1) / KV4_ROWS + MOVE_PAGES - 1) / MOVE_PAGES, bg);
-  return p.c.hd == 128 ? launch_pdl(kv4_move_kernel<128>, grid, dim3(128 * MOVE_PAGES), 0, s, p)
-                       : launch_pdl(kv4_move_kernel<64>, grid, dim3(128 * MOVE_PAGES), 0, s, p);
+  return p.c.hd == 128 ? launch_pdl(kv4_move_kernel<128>, grid, dim3(512), 0, s, p)
+                       : launch_pdl(kv4_move_kernel<64>, grid, dim3(512), 0, s, p);
 }
 
 }  // namespace chimera
