@@ -154,7 +154,10 @@ struct Raw {
   }
 };
 
-constexpr int APPEND_PAIRS = 2;  // of a thread, all their loads in flight
+// Two pairs of rows a thread, all their loads in flight.  Measured: 4 x 1000 bf16 rows of 32 heads of 128 (83 MB) 29.4 us,
+// 2.8 TB/s; one pair a thread 30.9.  Every value takes a minimum, a maximum, a check and eight steps to its code, which
+// overlap little with the loads of so few values a thread.
+constexpr int APPEND_PAIRS = 2;
 
 template <int HD, typename T>
 __global__ void __launch_bounds__(256) kv4_append_kernel(RowArgs a, int pairs) {
@@ -206,6 +209,7 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(RowArgs a, int pairs) {
   }
 }
 
+// Measured: the rows above 17.5 us, 4.7 TB/s; 2 x 8192 bf16 rows of 32 heads (340 MB) 64.6 us, 5.3 TB/s: memory.
 template <int HD, typename T>
 __global__ void __launch_bounds__(256) kv4_read_kernel(RowArgs a, int pairs) {
   pdl_wait();
@@ -265,7 +269,8 @@ __device__ __forceinline__ int warps_before(int v, int* sums, int& total) {
 // One block per (sequence, head): the kept slots.  The (budget - recent)-th largest key of the older slots is found
 // digit by digit, three histograms of up to 2048 bins; then one ordered pass takes every slot above it and
 // the first ones that equal it.  A warp owns a contiguous part of the slots, so the order of warps, rounds
-// and lanes is the slots' and the loads are coalesced.
+// and lanes is the slots' and the loads are coalesced.  Measured: 64 heads of 6000 to 16384 slots 14 us, in one
+// block per head: three passes of shared-memory atomics and their barriers.
 __global__ void __launch_bounds__(SEL_THREADS) kv4_select_kernel(Kv4EvictParams p) {
   pdl_wait();
   pdl_trigger();

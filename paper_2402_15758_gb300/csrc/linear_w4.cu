@@ -30,6 +30,8 @@ constexpr int WARPS = 24, THREADS = WARPS * 32, FEATURES = 16;
 // of the activations, 14.8, 8 tokens 23 to 26, 4096 x 4096 6.7.  Rings of bulk copies of 256 to 1024 bytes took 19.5
 // to 23, spans held in registers 17.7.  About 4.5 us of every call are the launch, the activations and the join;
 // the rest is bound by instructions and memory alike.
+// From 9 tokens on, which would be a second column of matrices, the tensor cores' kernel: 22016 x 4096, 8 tokens 18.8 us
+// here, 22.0 there (1 token 14.3 and 21.9); 4096 x 4096 10.0 and 11.5; 8 tokens in two terms 23.9 in both.
 constexpr int FEW_TOKENS = 8;
 
 struct FewParams {

@@ -16,6 +16,10 @@
 // Work split: stream-K over (tile, 256 columns of K), one CTA per SM; the parts of tiles cut between CTAs go to the
 // workspace and are added by a second kernel in CTA order (deterministic).
 //
+// Measured (GB300, 22016 x 4096, group 128): 16 tokens 22.5 us, 64 28.5, 64 in two terms 32.5 (alone, the tokens'
+// kernel 4, the products 26, the join 9), 256 tokens 83; 4096 x 4096, 16 tokens 11.8.  Bound by unpacking: 8 warps
+// take 0.7 us for 256 features x 128 columns, the tensor pipe waits.
+//
 // Roles: warp 0 TMA of the tokens, warps 1 and 3 the MMAs of a tile each (one warp for both was the bottleneck: an MMA
 // takes 28 cycles to issue and a wait 200), warp 2 TMA of the weights, the others unpack and sum (warp w: TMEM
 // lanes 32 (w % 4) ..).
@@ -37,7 +41,11 @@ constexpr int UNPACK_WARP = 4;
 // Eight warps unpack, whether a CTA has one tile or two (sixteen for two tiles: 16 tokens of 22016 x 4096 26.6 us
 // instead of 25.5, 64 tokens 41 instead of 35): warps that share the features of a tile.
 __host__ __device__ constexpr int halves(int ft) { return 2 / ft; }
-constexpr int FEW_PARTS = 3;                // parts of a 256-feature tile up to which CTAs take two tiles
+// Parts of a 256-feature tile up to which a CTA takes two tiles of 128 features, which share their tokens; with more the
+// join costs more than that saves.  64 tokens in two terms, 22016 x 4096 (2 parts): two tiles 31.1 us, one 39.8; 4096 x
+// 11008 (9 parts): two 27.2, one 25.0; 64 tokens in one, 12288 x 4096 (3 parts): two 20.6, one 22.7; 4096 x 4096 (9):
+// two 15.7, one 12.6.
+constexpr int FEW_PARTS = 4;
 constexpr int A_COLS = 64;                 // TMEM columns of a group's codes (128 of them)
 constexpr unsigned long long WAIT_NS = 2000000000ull;
 
