@@ -15,7 +15,7 @@
 // cut into blocks of 8 to 64; the pages are cut into parts, whose results the parts' cluster or a second kernel adds in
 // their order (no sum depends on who comes first).
 //
-// Measured (GB300, hd 128, times of calls in a graph): 1 query of 32 heads over 512 rows 7.2 us (launches, one trip to
+// Measured (GB300, hd 128, times of calls in a graph): 1 query of 32 heads over 512 rows 6.7 us (the launch, one trip to
 // memory after another, the join); over 16384 rows 30 us, 2.4 TB/s of 71 MB, bound by the instructions that turn codes
 // into numbers; 64 queries of 32 heads over 16384 rows 102 us: the tensor pipe is active 47 % of the time and an
 // instruction issued in 40 % (two warps per scheduler, 250 registers each, wait for one another's results).
@@ -246,12 +246,12 @@ struct Shape {
 };
 
 // Where the parts of a sequence meet: in a second kernel (and there are as many of each sequence, or they are dealt by
-// length), or, up to eight, in the cluster that their blocks form: as long on the device (1 query over 512 rows 7.2 us
-// either way), but one launch less for the host (a call 8.4 -> 6.8 us).
+// length), or, up to eight whose blocks are resident at once, in the cluster that these form: 1 query over 512 rows
+// 6.7 us instead of 7.3 on the device, and with one launch less 6.8 instead of 8.4 in the host's call.
 enum Parts { EQUAL, DEALT, CLUSTER };
 
 template <int HD, typename TQ, bool PRECISE, int NM, int RTW, Parts PARTS>
-__global__ void __launch_bounds__(WARPS * 32, NM == 1 ? 3 : 2) attn_kv4_kernel(const __grid_constant__ Kv4AttnParams p) {
+__global__ void __launch_bounds__(WARPS * 32, NM == 1 && PRECISE && PARTS != CLUSTER ? 3 : 2) attn_kv4_kernel(const __grid_constant__ Kv4AttnParams p) {
   extern __shared__ __align__(128) unsigned char smem[];
   using S = Shape<HD, PRECISE, NM, RTW>;
   using P = Kv4<HD>;
@@ -1001,7 +1001,10 @@ int blocks_of(const Kv4AttnParams& p) {
 int kv4_attn_blocks(const Kv4AttnParams& p) { return blocks_of(p); }
 
 namespace {
-int slots_of(const Cut& c) { return (c.nm == 1 ? 3 : 2) * tc_num_sms(); }  // blocks that are resident at once
+// Blocks that are resident at once (launch bounds): three of one matrix in two terms (1 query over 16384 rows 30.6 us,
+// with two blocks 32.0; 8 of 256 to 4096 rows 40 and 56); otherwise two, without spills (4 queries of groups of 4
+// heads, bf16 out, 16384 rows: 17.5 us, with three 20.5), and two in clusters (1 query over 512 rows: 6.7, 7.3).
+int slots_of(const Cut& c) { return (c.nm == 1 && c.precise ? 3 : 2) * tc_num_sms(); }
 size_t ws_floats(const Kv4AttnParams& p) {
   const size_t parts = p.slots ? static_cast<size_t>(blocks_of(p)) / p.c.B * p.slots : static_cast<size_t>(blocks_of(p)) * p.splits;
   return parts * cut_of(p).rows * (p.c.hd + 4);
@@ -1016,6 +1019,10 @@ void kv4_attn_split(Kv4AttnParams* p, int want, size_t most_floats) {
   const int most = std::min((p->c.max_pages + at_once - 1) / at_once, PARTS_MOST);
   p->slots = 0;
   p->splits = want ? want : std::max(1, std::min(slots_of(c) / blocks, most));
+  if (!want) {  // no more than it takes for as few rounds
+    const int rounds = (p->c.max_pages + p->splits * at_once - 1) / (p->splits * at_once);
+    p->splits = (p->c.max_pages + rounds * at_once - 1) / (rounds * at_once);
+  }
   while (p->splits > 1 && ws_floats(*p) > most_floats) --p->splits;
   if (want || p->c.B == 1 || p->c.B > DEAL_MOST || most == 1) return;
   p->least_pages = at_once;
@@ -1045,7 +1052,7 @@ template <int HD, typename TQ, bool PRECISE, int NM, int RTW>
 cudaError_t launch_attn(const Kv4AttnParams& p, cudaStream_t s) {
   if (p.slots) return launch_parts<HD, TQ, PRECISE, NM, RTW, DEALT>(p, s);
   if constexpr (RTW == 1)
-    if (p.splits > 1 && p.splits <= CLUSTER_MOST) return launch_parts<HD, TQ, PRECISE, NM, RTW, CLUSTER>(p, s);
+    if (p.splits > 1 && p.splits <= CLUSTER_MOST && blocks_of(p) * p.splits <= 2 * tc_num_sms()) return launch_parts<HD, TQ, PRECISE, NM, RTW, CLUSTER>(p, s);
   return launch_parts<HD, TQ, PRECISE, NM, RTW, EQUAL>(p, s);
 }
 template <int HD, typename TQ>
