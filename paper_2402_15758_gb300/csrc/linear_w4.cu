@@ -1,9 +1,8 @@
 // Linear with 4-bit weights: Y[M][N] (epilogue)= X[M][K] . W^T with
 // W[n][k] = scale[n][k / group] (code[n][k] - zero[n][k / group]), codes 0..15.
 //
-// A group's products are summed in fp32 by the matrix units; what its zero takes off and its scale follow in fp32,
-// from the group's sum of the activations:
-//   Y[m][n] = sum over groups of scale (sum code X - zero sum X).
+// code - zero is a whole number, exact in fp16; a group's products are summed in fp32 by the matrix units, and the
+// group's scale multiplies the sum, in fp32.
 // The activations enter as fp16, scaled by a power of two per token, hi + lo or fp32 ones as two fp16 terms (2^-23).
 #include <algorithm>
 
@@ -22,14 +21,18 @@ constexpr int WARPS = 24, THREADS = WARPS * 32, FEATURES = 16;
 // One CTA of 24 warps per SM.  A tile is 16 features (the MMA's rows); KS warps share its K by spans of four groups
 // and join their sums after `join` tiles or at the end.  A lane copies (cp.async) into shared memory exactly what it
 // will read itself, so a warp runs ahead of its loads with no barrier at all.  The activations stay in shared memory
-// for the whole launch.  A nibble is used where it lies: at the end of a mantissa with exponent 0 it is a (subnormal)
-// fp16 number, so 8 codes cost 5 instructions; nibbles at bit 4 count 16 times, in sums of their own.
+// for the whole launch.
 //
-// Measured (GB300, 22016 x 4096, group 128, 47 MB): one token 14.4 us, 3.3 TB/s; 8 tokens 18.8; 4096 x 4096 5.9 us.
-// With codes converted to fp16 numbers (9 instructions) 15.2; with three CTAs of 8 warps, each with its own copy
-// of the activations, 14.8, 8 tokens 23 to 26, 4096 x 4096 6.7.  Rings of bulk copies of 256 to 1024 bytes took 19.5
-// to 23, spans held in registers 17.7.  About 4.5 us of every call are the launch, the activations and the join;
-// the rest is bound by instructions and memory alike.
+// TINY, where the result is rounded to bf16 and groups are longer than 32: a nibble is used where it lies.  At the end of
+// a mantissa with exponent 0 it is a (subnormal) fp16 number, so 8 codes cost 5 instructions instead of 9; nibbles at bit
+// 4 count 16 times, in sums of their own; the zero follows in fp32, from the group's sum of the activations.  Sums of
+// codes without their zero are longer: the error is 2e-6 of the result instead of 2e-7, which fp32 results do without
+// (and sums of 32 cost more than they save: 23.1 us instead of 22.4).
+//
+// Measured (GB300, 22016 x 4096, group 128, 47 MB): one token 14.3 us, 3.3 TB/s, fp32 out 15.2, in two terms 17.8;
+// 8 tokens 19; 4096 x 4096 5.9 us.  Three CTAs of 8 warps, each with its own copy of the activations: 8 tokens 23 to 26,
+// 4096 x 4096 6.7.  Rings of bulk copies of 256 to 1024 bytes took 19.5 to 23, spans held in registers 17.7.  About
+// 4.5 us of every call are the launch, the activations and the join; the rest is bound by issue slots and the math pipe.
 // From 9 tokens on, which would be a second column of matrices, the tensor cores' kernel: 22016 x 4096, 8 tokens 18.8 us
 // here, 22.0 there (1 token 14.3 and 21.9); 4096 x 4096 10.0 and 11.5; 8 tokens in two terms 23.9 in both.
 constexpr int FEW_TOKENS = 8;
@@ -41,7 +44,7 @@ struct FewParams {
   int join;            // tiles whose sums are held
   int x_pitch;         // of a token's term
   int pairs;           // ceil(M / 2): lanes of a row that hold tokens
-  int at_x, at_sums_x, at_sums;   // offsets in shared memory
+  int at_x, at_sums_x, at_sums;  // offsets in shared memory
 };
 
 // The scale of a token whose largest magnitude is 2^-6 to 2^7 is 2^8 without asking, so one pass over
@@ -118,7 +121,7 @@ __device__ __forceinline__ void swap_near(uint4& v, int t) {
   v = up ? make_uint4(x, v.y, y, v.w) : make_uint4(v.x, x, v.z, y);
 }
 
-template <int G, int TERMS>
+template <int G, int TERMS, bool TINY>
 __global__ void __launch_bounds__(THREADS, 1) w4_few_kernel(const __grid_constant__ FewParams p) {
   extern __shared__ __align__(128) unsigned char smem[];  // the warps' rings, activations, sums
   __shared__ uint32_t sh_top[FEW_TOKENS];
@@ -177,6 +180,7 @@ __global__ void __launch_bounds__(THREADS, 1) w4_few_kernel(const __grid_constan
     unsigned char* dst = smem + p.at_x + m * TERMS * p.x_pitch + i / 16 * 256 + (at * 4 + th) * 16;
     *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
     if (TERMS == 2) *reinterpret_cast<uint4*>(dst + p.x_pitch) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    if (!TINY) return;
     // the group's sum, of what the matrix units will be given
     float sum = 0.f;
 #pragma unroll
@@ -262,7 +266,7 @@ __global__ void __launch_bounds__(THREADS, 1) w4_few_kernel(const __grid_constan
       const float v[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (2 * t + (i & 1) < w.M && n + 8 * (i >> 1) < w.N) store_y(w, 2 * t + (i & 1), n + 8 * (i >> 1), v[i] * (1.f / CODE_UNIT) * down[i & 1]);
+        if (2 * t + (i & 1) < w.M && n + 8 * (i >> 1) < w.N) store_y(w, 2 * t + (i & 1), n + 8 * (i >> 1), v[i] * (TINY ? 1.f / CODE_UNIT : 1.f) * down[i & 1]);
     }
     meet();
     first_tile += held * step;
@@ -294,36 +298,57 @@ __global__ void __launch_bounds__(THREADS, 1) w4_few_kernel(const __grid_constan
         if (G < 128) swap_far(va, t), swap_far(vb, t);
         if (G < 64) swap_near(va, t), swap_near(vb, t);
         const uint32_t a[4] = {va.x, va.y, va.z, va.w}, b[4] = {vb.x, vb.y, vb.z, vb.w};
-        const uint32_t both_a = bf16_bits(now.za) | now.sa, both_b = bf16_bits(now.zb) | now.sb;
-        float sa, sb, za, zb, low[4], high[4];  // products of the low and the high nibbles of a group's bytes
+        const uint32_t both_a = (TINY ? bf16_bits(now.za) : now.za << 16) | now.sa, both_b = (TINY ? bf16_bits(now.zb) : now.zb << 16) | now.sb;
+        float sa, sb, za, zb, low[4], high[4];  // sums of products; with nibbles as they lie, high: of those that count 16 times
         float2 sum_x;
+        uint32_t oa, oa16, ob, ob16;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
           if (v % BLOCKS == 0) {  // a new group
             const int g = i * (4 / BLOCKS) + v / BLOCKS;
             const uint32_t ga = __shfl_sync(0xffffffffu, both_a, (lane & ~3) | g), gb = __shfl_sync(0xffffffffu, both_b, (lane & ~3) | g);
             sa = __uint_as_float(ga << 16), sb = __uint_as_float(gb << 16);
-            za = __uint_as_float(ga & 0xffff0000u), zb = __uint_as_float(gb & 0xffff0000u);
-            sum_x = *reinterpret_cast<const float2*>(sums_x + (span * 4 + g) * FEW_TOKENS + 2 * t);
+            if constexpr (TINY) {
+              za = __uint_as_float(ga & 0xffff0000u), zb = __uint_as_float(gb & 0xffff0000u);
+              sum_x = *reinterpret_cast<const float2*>(sums_x + (span * 4 + g) * FEW_TOKENS + 2 * t);
+            } else {
+              oa = zero_off(ga >> 16), oa16 = zero_off16(ga >> 16), ob = zero_off(gb >> 16), ob16 = zero_off16(gb >> 16);
+            }
           }
           uint32_t ua[4], ub[4];
-          codes_tiny(a[v], ua);
-          codes_tiny(b[v], ub);
+          if constexpr (TINY) {
+            codes_tiny(a[v], ua);
+            codes_tiny(b[v], ub);
+          } else {
+            w4_codes_f16(a[v], oa, oa16, ua);
+            w4_codes_f16(b[v], ob, ob16, ub);
+          }
 #pragma unroll
           for (int s = 0; s < TERMS; ++s) {
             const uint4 x = *reinterpret_cast<const uint4*>(xb + i * 256 + s * p.x_pitch + v * 64);
-            if (v % BLOCKS == 0 && s == 0) {
-              mma_f16_first(low, ua[0], ub[0], ua[2], ub[2], x.x, x.z);
-              mma_f16_first(high, ua[1], ub[1], ua[3], ub[3], x.y, x.w);
+            const bool fresh = v % BLOCKS == 0 && s == 0;
+            if constexpr (TINY) {
+              if (fresh) {
+                mma_f16_first(low, ua[0], ub[0], ua[2], ub[2], x.x, x.z);
+                mma_f16_first(high, ua[1], ub[1], ua[3], ub[3], x.y, x.w);
+              } else {
+                mma_f16(low, ua[0], ub[0], ua[2], ub[2], x.x, x.z);
+                mma_f16(high, ua[1], ub[1], ua[3], ub[3], x.y, x.w);
+              }
             } else {
-              mma_f16(low, ua[0], ub[0], ua[2], ub[2], x.x, x.z);
-              mma_f16(high, ua[1], ub[1], ua[3], ub[3], x.y, x.w);
+              if (fresh)
+                mma_f16_first(low, ua[0], ub[0], ua[1], ub[1], x.x, x.y);
+              else
+                mma_f16(low, ua[0], ub[0], ua[1], ub[1], x.x, x.y);
+              mma_f16(low, ua[2], ub[2], ua[3], ub[3], x.z, x.w);
             }
           }
           if (v % BLOCKS == BLOCKS - 1) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              acc[j] = fmaf(j < 2 ? sa : sb, fmaf(high[j], 0.0625f, fmaf(j < 2 ? -za : -zb, j & 1 ? sum_x.y : sum_x.x, low[j])), acc[j]);
+            for (int j = 0; j < 4; ++j) {
+              if (TINY) low[j] = fmaf(high[j], 0.0625f, fmaf(j < 2 ? -za : -zb, j & 1 ? sum_x.y : sum_x.x, low[j]));
+              acc[j] = fmaf(j < 2 ? sa : sb, low[j], acc[j]);
+            }
           }
         }
       }
@@ -334,14 +359,17 @@ __global__ void __launch_bounds__(THREADS, 1) w4_few_kernel(const __grid_constan
   if (held) join();
 }
 
-template <int G, int TERMS>
+template <int G, int TERMS, bool TINY>
 cudaError_t launch_few(const FewParams& p, size_t smem, int grid, cudaStream_t s) {
-  const cudaError_t e = allow_smem<w4_few_kernel<G, TERMS>>(226 * 1024);
-  return e != cudaSuccess ? e : launch_pdl(w4_few_kernel<G, TERMS>, dim3(grid), dim3(THREADS), smem, s, p);
+  const cudaError_t e = allow_smem<w4_few_kernel<G, TERMS, TINY>>(226 * 1024);
+  return e != cudaSuccess ? e : launch_pdl(w4_few_kernel<G, TERMS, TINY>, dim3(grid), dim3(THREADS), smem, s, p);
 }
 template <int G>
 cudaError_t launch_few_terms(const FewParams& p, size_t smem, int grid, cudaStream_t s) {
-  return p.w.x_f32 || p.w.X_lo ? launch_few<G, 2>(p, smem, grid, s) : launch_few<G, 1>(p, smem, grid, s);
+  const bool two = p.w.x_f32 || p.w.X_lo;
+  if constexpr (G > 32)
+    if (!p.w.out_f32) return two ? launch_few<G, 2, true>(p, smem, grid, s) : launch_few<G, 1, true>(p, smem, grid, s);
+  return two ? launch_few<G, 2, false>(p, smem, grid, s) : launch_few<G, 1, false>(p, smem, grid, s);
 }
 
 // Shared memory of the plan, 0 when the activations do not fit.

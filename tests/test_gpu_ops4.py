@@ -100,6 +100,26 @@ def test_linear_w4(M, N, K, group, kind):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bf16", "split", "fp32"])
+@pytest.mark.parametrize("M,N,K,group", [(1, 4096, 12288, 128), (3, 1028, 11488, 32), (8, 700, 2592, 64), (40, 700, 8192, 128)])
+def test_linear_w4_fp32_results_keep_their_bits(M, N, K, group, kind):
+    # Two fp16 terms hold an activation to 2^-22, and a chain of 16 sums that each cut off 2^-24 of a group's sum, always
+    # toward zero, can add 2^-20 at worst; independent groups average that to well under 2^-21 in the norm.
+    g = _gen(M, N, K, 5)
+    W, scale, zero, dense = _weights(g, N, K, group, True)
+    x, lo = _normal(g, M, K), None
+    value = x.double()
+    if kind != "fp32":
+        hi = x.to(torch.bfloat16)
+        lo = (x - hi.float()).to(torch.bfloat16) if kind == "split" else None
+        x, value = hi, hi.double() + (lo.double() if lo is not None else 0.0)
+    Y = torch.zeros(M, N, device="cuda")
+    pkg.op_linear_w4(x, W, scale, Y, zeros=zero, group=group, out_f32=True, X_lo=lo)
+    ref = value @ dense.T
+    assert float((Y.double() - ref).norm() / ref.norm()) <= 2.0 ** -22 + 2.0 ** -21
+
+
+@pytest.mark.gpu
 def test_linear_w4_extreme_activations():
     # a token that is not finite spoils its own row alone; very large and very small ones keep their precision
     g = _gen(7)
