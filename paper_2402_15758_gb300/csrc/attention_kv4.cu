@@ -515,13 +515,14 @@ __global__ void __launch_bounds__(WARPS * 32, NM == 1 && PRECISE && PARTS != CLU
             wf[h][x][i] = pack_f16(w[0], w[1]);
             wf[h][x][2 + i] = pack_f16(w[2], w[3]);
             // The sums take the weights as they were rounded: the row stays an average of its values, and a key that
-            // takes nearly all of it gives its value without the rounding.
+            // takes nearly all of it gives its value without the rounding.  (Not those below fp16's normal numbers,
+            // which the products hardly notice: a key of much weight and small values counts in the sums all the same.)
             const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&wf[h][x][i]));
             const float2 c = __half22float2(*reinterpret_cast<const __half2*>(&wf[h][x][2 + i]));
             const float rounded[4] = {a.x, a.y, c.x, c.y};
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-              if (step[h][j] * inv_top > 0x1p-100f) e[j] = rounded[j] * inverse[h][j];
+              if (w[j] >= 0x1p-14f) e[j] = rounded[j] * inverse[h][j];
           }
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
