@@ -5,8 +5,8 @@
 //   o   = sum_j p_j v_j      = sum_j (p_j s_j) c'_j + sum_j p_j b'_j
 // so both matrix products take the codes as whole fp16 numbers straight from the packed words.
 // The factors that are no whole numbers enter as fp16 terms: a query row is first scaled by a power of two to a largest
-// value in [16, 32) and is two terms, hi + lo (22 bits); p s is divided by the largest step seen so far (a power of two
-// above it) and is two terms, or one where the result is rounded to bf16 anyway (Shape).  Of two terms, the 16 rows of
+// value in [16, 32) and is two terms, hi + lo (22 bits); p s is divided by a power of two of the row's own (UNITS below)
+// and is two terms, or one where the result is rounded to bf16 anyway (Shape).  Of two terms, the 16 rows of
 // a matrix product are those of 8 query rows, and both terms of a row end in the same thread.
 //
 // A warp takes whole pages (16 keys).  Its copies are one bulk copy per page into a ring of its own (or of the
@@ -17,8 +17,8 @@
 //
 // Measured (GB300, hd 128, times of calls in a graph): 1 query of 32 heads over 512 rows 6.7 us (the launch, one trip to
 // memory after another, the join); over 16384 rows 30 us, 2.4 TB/s of 71 MB, bound by the instructions that turn codes
-// into numbers; 64 queries of 32 heads over 16384 rows 102 us: the tensor pipe is active 47 % of the time and an
-// instruction issued in 40 % (two warps per scheduler, 250 registers each, wait for one another's results).
+// into numbers; 64 queries of 32 heads over 16384 rows 105 us (before the rows had units of their own 103: the tensor pipe was
+// active 47 % of the time and an instruction issued in 40 % two warps per scheduler, 250 registers each, wait for one another's results).
 #include <algorithm>
 
 #include "kernels.h"
@@ -35,6 +35,12 @@ constexpr float LOG2E = 1.4426950408889634f;
 // logit exceeds it by more than 15: weights of up to 2^15 leave the fp16 pairs an absolute error
 // of 2^-36 of the largest (many keys of little weight add up to the result).
 constexpr float BELOW = 11.f, SLACK = 15.f;
+// UNITS.  A row's sums are held in a power of two of its own, at least LEAST_UNIT.  It is above every step that the row
+// has seen (then p s stays below 2^15), unless that is more than 16 times its largest p s: a key of little weight takes
+// the others no bits, however large its values are.  What a row does not see takes no part in it.  Bases count as steps 2^-40
+// times as large, which only those of equal or enormous values notice.
+constexpr float LEAST_UNIT = 0x1p-96f;  // (weights over units stay within fp32)
+__device__ __forceinline__ float step_size(float step, float base) { return fmaxf(step, 0x1p-40f * fabsf(base)); }
 constexpr unsigned long long WAIT_NS = 2000000000ull;
 
 // 2^x, relative error 2^-22; results below 2^-126 are 0.
@@ -43,6 +49,9 @@ __device__ __forceinline__ float pow2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// 1 / x of a power of two from 2^-126 to 2^126.
+__device__ __forceinline__ float one_over(uint32_t bits) { return __uint_as_float(0x7f000000u - bits); }
+__device__ __forceinline__ float one_over(float x) { return one_over(__float_as_uint(x)); }
 __device__ __forceinline__ float quad_sum(float x) {
   x += __shfl_xor_sync(0xffffffffu, x, 1);
   return x + __shfl_xor_sync(0xffffffffu, x, 2);
@@ -242,7 +251,8 @@ struct Shape {
   static constexpr bool HELD = PRECISE && NM == 1;
   static constexpr int TERMS = PRECISE ? 1 : 2;
   static constexpr int FRAGS = ML + WARPS * TILE * 8;
-  static constexpr int BYTES = FRAGS + (HELD ? 0 : RTW * NM * TERMS * (HD / 16) * 512);
+  static constexpr int PEAKS = FRAGS + (HELD ? 0 : RTW * NM * TERMS * (HD / 16) * 512);
+  static constexpr int BYTES = PEAKS + WARPS * 32 * NM * (PRECISE ? 1 : 2) * 4;  // of a thread's rows
 };
 
 // Where the parts of a sequence meet: in a second kernel (and there are as many of each sequence, or they are dealt by
@@ -360,10 +370,14 @@ __global__ void __launch_bounds__(WARPS * 32, NM == 1 && PRECISE && PARTS != CLU
   if (!S::HELD) __syncthreads();
 
   float o[NM][HD / 8][4] = {};
-  float m[NR], l[NR], bs[NR];  // l and bs: this thread's keys alone
+  float m[NR], l[NR], bs[NR];  // l and bs: of p and p b', this thread's keys alone
 #pragma unroll
   for (int i = 0; i < NR; ++i) m[i] = NONE, l[i] = bs[i] = 0.f;
-  float top = 0x1p-126f, inv_top = 0x1p126f;  // power of two above every V step so far
+  float inv_unit[NR];  // one over the row's unit
+  float* peak = reinterpret_cast<float*>(smem + S::PEAKS) + tid;  // the largest p s of a row's raises (registers are short)
+#pragma unroll
+  for (int i = 0; i < NR; ++i) inv_unit[i] = 1.f / LEAST_UNIT, peak[i * WARPS * 32] = 0.f;
+  float least_unit = LEAST_UNIT;  // of this thread's rows
   int stage = 0;
   uint32_t phase = 0;
   for (int k = 0; k < mine; k += PAGES) {
@@ -436,48 +450,61 @@ __global__ void __launch_bounds__(WARPS * 32, NM == 1 && PRECISE && PARTS != CLU
       }
       key_scales(page[h] + P::VS, t, step[h], base[h]);
       const int slot0 = (p0 + slice + (k + h) * S::SLICES) * KV4_ROWS;
-      if (slot0 + KV4_ROWS > all.n || (h && !two)) {  // a hidden key counts nothing, whatever its codes and steps are
+      if (slot0 + KV4_ROWS > all.n || (h && !two)) {
+        // A hidden key counts nothing, whatever its codes, steps and bases are.  A row of V without numbers has the weight 0
+        // in the products, and makes those sums that see it no number.
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int slot = slot0 + 2 * t + (j & 1) + 8 * (j >> 1);
-          const bool held = slot < all.total && !(h && !two);
-          if (!held) step[h][j] = base[h][j] = 0.f;
+          const bool held = slot < all.total && !(h && !two), number = isfinite(step[h][j]) && isfinite(base[h][j]);
 #pragma unroll
-          for (int i = 0; i < NR; ++i)
-            if (!held || (slot >= all.n && !(local[i] >> (slot - all.n) & 1))) z[h][i][j] = -INFINITY;
+          for (int i = 0; i < NR; ++i) {
+            if (!held || (slot >= all.n && !(local[i] >> (slot - all.n) & 1)))
+              z[h][i][j] = -INFINITY;
+            else if (!number)
+              bs[i] = NAN;
+          }
+          if (!held || !number) step[h][j] = base[h][j] = 0.f;
         }
       }
 #pragma unroll
+      for (int j = 0; j < 4; ++j) smax = fmaxf(smax, step_size(step[h][j], base[h][j]));
+#pragma unroll
       for (int i = 0; i < NR; ++i) zmax[i] = fmaxf(zmax[i], fmaxf(fmaxf(z[h][i][0], z[h][i][1]), fmaxf(z[h][i][2], z[h][i][3])));
-      smax = fmaxf(smax, fmaxf(fmaxf(step[h][0], step[h][1]), fmaxf(step[h][2], step[h][3])));
     }
-    bool raise = smax > top;
+    bool raise = smax > least_unit;
 #pragma unroll
     for (int i = 0; i < NR; ++i) raise = raise || zmax[i] > m[i] + SLACK;
     if (__any_sync(0xffffffffu, raise)) {
-      float wide = smax;
-#pragma unroll
-      for (int x = 16; x; x >>= 1) wide = fmaxf(wide, __shfl_xor_sync(0xffffffffu, wide, x));
-      float shrink = 1.f;
-      if (wide > top) {
-        const uint32_t e = min((__float_as_uint(wide) >> 23) + 1, 252u);
-        const float was = top;
-        top = __uint_as_float(e << 23);
-        inv_top = __uint_as_float((254 - e) << 23);
-        shrink = was * inv_top;
-      }
+      least_unit = INFINITY;
 #pragma unroll
       for (int x = 0; x < NM; ++x) {
         float a[RM];
 #pragma unroll
         for (int i = 0; i < RM; ++i) {
           const int at = x * RM + i;
-          const float raised = fmaxf(m[at], quad_max(zmax[at]) - BELOW);
+          const float raised = fmaxf(m[at], quad_max(zmax[at]) - BELOW), unit = one_over(inv_unit[at]);
+          float wide = 0.f, most = 0.f;  // the largest step that the row sees, and p s
+#pragma unroll
+          for (int h = 0; h < PAGES; ++h) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float size = step_size(step[h][j], base[h][j]);
+              if (z[h][at][j] > -INFINITY) wide = fmaxf(wide, size);
+              most = fmaxf(most, pow2(z[h][at][j] - raised) * size);
+            }
+          }
+          wide = quad_max(wide);
           a[i] = exp2f(m[at] - raised);
           m[at] = raised;
-          l[at] *= a[i];
+          most = fmaxf(peak[at * WARPS * 32] * a[i], quad_max(most));
+          peak[at * WARPS * 32] = most;
+          const float wanted = fmaxf(fminf(wide > unit ? fminf(2.f * wide, 0x1p125f) : unit, 16.f * most), LEAST_UNIT);
+          inv_unit[at] = one_over(__float_as_uint(wanted) & 0xff800000u);
+          least_unit = fminf(least_unit, one_over(inv_unit[at]));
+          l[at] = l[at] * a[i] * unit * inv_unit[at];  // (step by step: weights count whatever became of the unit)
+          a[i] = a[i] * unit * inv_unit[at];           // the sums so far, in the new unit
           bs[at] *= a[i];
-          a[i] *= shrink;
         }
 #pragma unroll
         for (int j = 0; j < HD / 8; ++j) {
@@ -492,7 +519,7 @@ __global__ void __launch_bounds__(WARPS * 32, NM == 1 && PRECISE && PARTS != CLU
 #pragma unroll
       for (int h = 0; h < PAGES; ++h) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) inverse[h][j] = __fdividef(1.f, step[h][j] * inv_top);
+        for (int j = 0; j < 4; ++j) inverse[h][j] = __fdividef(1.f, step[h][j]);
       }
     }
 #pragma unroll
@@ -506,7 +533,8 @@ __global__ void __launch_bounds__(WARPS * 32, NM == 1 && PRECISE && PARTS != CLU
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             e[j] = pow2(z[h][at][j] - m[at]);
-            w[j] = e[j] * (step[h][j] * inv_top);
+            e[j] *= inv_unit[at];
+            w[j] = e[j] * step[h][j];
           }
           if (PRECISE) {
             split_f16(w[0], w[1], wf[h][x][0], wf[h][x][1]);
@@ -609,7 +637,8 @@ __global__ void __launch_bounds__(WARPS * 32, NM == 1 && PRECISE && PARTS != CLU
       for (int i = 0; i < RM; ++i) {
         const float* d = o[x][j];
         *reinterpret_cast<float2*>(sums + ((PRECISE ? 8 : 16) * x + r + 8 * i) * S::PITCH + 8 * j + 2 * t) =
-            make_float2(fmaf(PRECISE ? d[0] + d[2] : d[2 * i], top, bs[x * RM + i]), fmaf(PRECISE ? d[1] + d[3] : d[2 * i + 1], top, bs[x * RM + i]));
+            make_float2(((PRECISE ? d[0] + d[2] : d[2 * i]) + bs[x * RM + i]) * one_over(inv_unit[x * RM + i]),
+                        ((PRECISE ? d[1] + d[3] : d[2 * i + 1]) + bs[x * RM + i]) * one_over(inv_unit[x * RM + i]));
       }
     }
   }
@@ -617,7 +646,7 @@ __global__ void __launch_bounds__(WARPS * 32, NM == 1 && PRECISE && PARTS != CLU
   for (int i = 0; i < NR; ++i)
     if (t == 0) {  // rows r, r + 8, .. of the tile
       ml[(warp * TILE + r + 8 * i) * 2] = m[i];
-      ml[(warp * TILE + r + 8 * i) * 2 + 1] = l[i];
+      ml[(warp * TILE + r + 8 * i) * 2 + 1] = l[i] * one_over(inv_unit[i]);
     }
   __syncthreads();
 
@@ -978,8 +1007,8 @@ cudaError_t launch_sized(size_t smem, dim3 grid, const Kv4AttnParams& p, cudaStr
 }  // namespace
 
 // How a call's rows are cut: one term per weight where the result is rounded to bf16 alone and there are rows enough
-// to fill a matrix with them (32 heads over 16384 rows, 64 queries 102 us, with two terms 146; 16 queries 41.8 and
-// 43.7); two matrices per warp from there on, and warps that share pages for more rows (with one matrix and no
+// to fill a matrix with them (32 heads over 16384 rows, 64 queries 105 us, with two terms 153; 16 queries 40.8 and
+// 45.2); two matrices per warp from there on, and warps that share pages for more rows (with one matrix and no
 // sharing: 143 and 287 us, 16 queries 41.9 and 51.7).
 namespace {
 struct Cut {

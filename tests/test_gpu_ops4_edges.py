@@ -1,11 +1,12 @@
 """The 4-bit operators at the edges of their range.  Tolerances are those of test_gpu_ops4.py."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
 import paper_2402_15758_gb300 as pkg
-from test_gpu_ops4 import BF16_TOL, Cache, _anc, _gen, _ints, _normal, _probabilities, _rel_rows, _stands_for
+from test_gpu_ops4 import ATT_TOL, BF16_TOL, Cache, _anc, _gen, _ints, _masks, _normal, _probabilities, _rel_rows, _stands_for
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -35,6 +36,69 @@ def _reference(cache, q, ctx, masks, nq, n_local, H):
         out.append((torch.softmax(z, -1).nan_to_num(0.0) @ v).transpose(0, 1))
         lse.append(torch.logsumexp(z, -1).T)
     return torch.stack(out), torch.stack(lse)
+
+
+def _spoil(cache, b, slot, word):
+    """The step and base (the halves of `word`) of a slot's K and V, and all of its K codes, in every head."""
+    at, row = 16 * cache.hd + 4 * (slot % 16), slot % 16
+    page = cache.pool[int(cache.table[b, slot // 16])]
+    four = torch.from_numpy(np.array([word], dtype=np.uint32).view(np.uint8)).cuda()
+    page[:, at:at + 4] = four
+    page[:, at + 64:at + 68] = four
+    page[:, row * cache.hd // 2:(row + 1) * cache.hd // 2] = 255
+
+
+#    ctx per sequence   G   H   hd  nq  n_local
+HIDDEN = [([20], 2, 4, 128, 5, 5), ([0], 1, 1, 64, 3, 3), ([513], 4, 32, 64, 1, 4), ([300, 77], 8, 8, 128, 64, 64),
+          ([1000], 4, 4, 128, 33, 40), ([1900, 0, 17], 40, 40, 128, 2, 3), ([700, 3, 1500, 64], 16, 16, 64, 40, 40)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", HIDDEN)
+@pytest.mark.parametrize("word", [0xffffffff, 0x7f807f80, 0xff80ff80, 0x00007e00, 0x7e007e00], ids=["nan", "inf", "-inf", "step", "large"])
+@pytest.mark.parametrize("form", ["f32", "pair", "bf16"])
+def test_hidden_local_rows_are_no_part_of_a_result(case, word, form):
+    ctx, G, H, hd, nq, n_local = case
+    g, r = _gen(41, len(ctx), G, nq), np.random.default_rng(41)
+    cache = Cache(g, [n + n_local for n in ctx], G, hd)
+    masks = _masks("tree", n_local, r)
+    q = _normal(g, len(ctx) * nq, H * hd) * 1.5
+    ref, lse_ref = _reference(cache, q, ctx, masks, nq, n_local, H)
+    bad = sorted({n_local - 1, n_local // 2, n_local // 3} - {0})
+    for b in range(len(ctx)):
+        for j in bad:
+            _spoil(cache, b, ctx[b] + j, word)
+    clean = [i for i in range(nq) if not any(masks[i] >> j & 1 for j in bad)]
+    assert clean  # the root at least
+    for splits in (0, 1, 3):
+        got, lse = _attend(cache, q, ctx, masks, nq, n_local, H, form, splits)
+        assert _rel_rows(got[:, clean], ref[:, clean]) <= (BF16_TOL if form == "bf16" else ATT_TOL)
+        if lse is not None:
+            assert float((lse.double() - lse_ref)[:, clean].abs().max()) <= ATT_TOL * 10
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", ["f32", "pair", "bf16"])
+@pytest.mark.parametrize("nq", [3, 24])
+def test_a_row_without_numbers_reaches_those_that_see_it_alone(form, nq):
+    # appended as the library does it: V of local row 1 holds an infinity
+    ctx, G, H, hd = [90], 2, 4, 128
+    g = _gen(43, nq)
+    cache = Cache(g, [90 + nq], G, hd)
+    masks = [1] + [1 | 1 << i for i in range(1, nq)]  # children of the root
+    q = _normal(g, nq, H * hd)
+    ref, lse_ref = _reference(cache, q, ctx, masks, nq, nq, H)
+    k, v = _normal(g, 1, G * hd), _normal(g, 1, G * hd)
+    v[:, [5, hd + 5]] = float("inf")
+    pkg.op_kv4_append(k, v, cache.pool, cache.table, _ints([91]), 1, hd)
+    cache.k[0, 91] = _stands_for(k.view(G, hd))
+    lse_ref[:, 1] = _reference(cache, q, ctx, masks, nq, nq, H)[1][:, 1]
+    got, lse = _attend(cache, q, ctx, masks, nq, nq, H, form)
+    rest = [i for i in range(nq) if i != 1]
+    assert torch.isnan(got[:, 1]).all()
+    assert _rel_rows(got[:, rest], ref[:, rest]) <= (BF16_TOL if form == "bf16" else ATT_TOL)
+    if lse is not None:
+        assert float((lse.double() - lse_ref).abs().max()) <= ATT_TOL * 10
 
 
 def _one_key(cache, q, at, logit, size):
@@ -68,3 +132,51 @@ def test_a_small_row_of_much_weight(size, at, nq):
     for splits in (0, 1):
         got, _ = _attend(cache, q, [300], [0] * nq, nq, 0, H, "bf16", splits)
         assert _rel_rows(got, ref) <= BF16_TOL
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", ["f32", "pair", "bf16"])
+@pytest.mark.parametrize("size", [1e6, 1e12, 1e15])
+@pytest.mark.parametrize("at,nq", [(3, 1), (3, 40), (299, 2), (299, 40), (150, 9)])
+def test_a_large_row_of_little_weight(form, size, at, nq):
+    # its weight, exp(-60) of the others', times its size is nothing beside them
+    G, H, hd = 2, 4, 128
+    g = _gen(47, at, nq)
+    cache = Cache(g, [300], G, hd)
+    q = _alike(g, nq, H, G, hd)
+    _one_key(cache, q, at, -60.0, size)
+    ref, _ = _reference(cache, q, [300], [0] * nq, nq, 0, H)
+    for splits in (0, 1):
+        got, _ = _attend(cache, q, [300], [0] * nq, nq, 0, H, form, splits)
+        assert _rel_rows(got, ref) <= (BF16_TOL if form == "bf16" else ATT_TOL)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", ["f32", "pair", "bf16"])
+@pytest.mark.parametrize("nq", [2, 40])
+@pytest.mark.parametrize("size", [1e-26, 1e-9, 1.0, 1e12, 1e30])
+def test_rows_of_equal_values_among_others(form, nq, size):
+    # rows of equal values have step 0; a zero row, and one of 1e20 times the others' size, which all others vanish beside
+    G, H, hd = 2, 4, 64
+    g = _gen(53, nq)
+    cache = Cache(g, [200], G, hd)
+    q = _normal(g, nq, H * hd)
+    v = _normal(g, 200, G, hd)
+    v[::3] = v[::3, :, :1]
+    v[5:40] = 0
+    at = [s for s in range(200) if s % 3 == 0]
+    for large in (False, True):
+        if large and size > 1e15:
+            continue
+        x = v * size
+        if large:
+            x[at[-4]] = 1e20 * size
+        pkg.op_kv4_append(cache.k[0].float().reshape(200, -1), x.view(200, -1), cache.pool, cache.table, _ints([0]), 200, hd)
+        cache.k[0], cache.v[0] = _stands_for(cache.k[0]), _stands_for(x)
+        ref, _ = _reference(cache, q, [200], [0] * nq, nq, 0, H)
+        for splits in (0, 1):
+            got, _ = _attend(cache, q, [200], [0] * nq, nq, 0, H, form, splits)
+            assert _rel_rows(got, ref) <= (BF16_TOL if form == "bf16" else ATT_TOL)
+    pkg.op_kv4_append(cache.k[0].float().reshape(200, -1), torch.zeros(200, G * hd, device="cuda"), cache.pool, cache.table, _ints([0]),
+                      200, hd)
+    assert (_attend(cache, q, [200], [0] * nq, nq, 0, H, form)[0] == 0).all()
