@@ -143,17 +143,20 @@ struct Seen {
   }
 };
 
-__device__ __forceinline__ Seen what_is_seen(const Kv4AttnParams& p, int b) {
+// Of sequence b, within what its page table holds; `fits` says whether n_ctx was.
+__device__ __forceinline__ Seen rows_of(const Kv4AttnParams& p, int b, bool& fits) {
+  const int cap = p.c.max_pages * KV4_ROWS, n = p.n_ctx[b];
   Seen s;
-  int n = p.n_ctx[b];
-  const int cap = p.c.max_pages * KV4_ROWS;
-  if (n < 0 || n + p.n_local > cap) {
-    if (threadIdx.x == 0) atomicOr(p.c.err, ERR_CAPACITY);
-    n = min(max(n, 0), max(cap - p.n_local, 0));
-  }
-  s.n = n;
-  s.total = min(n + p.n_local, cap);
+  fits = n >= 0 && n <= cap - p.n_local;  // (a sum with any n_ctx could pass 32 bits)
+  s.n = fits ? n : min(max(n, 0), max(cap - p.n_local, 0));
+  s.total = min(s.n + p.n_local, cap);
   s.local = 0;
+  return s;
+}
+__device__ __forceinline__ Seen what_is_seen(const Kv4AttnParams& p, int b) {
+  bool fits;
+  const Seen s = rows_of(p, b, fits);
+  if (!fits && threadIdx.x == 0) atomicOr(p.c.err, ERR_CAPACITY);
   return s;
 }
 
@@ -168,9 +171,9 @@ struct Deal {
   int parts, first;
 };
 __device__ __forceinline__ Deal deal_slots(const Kv4AttnParams& p, int lane) {
-  const int cap = p.c.max_pages * KV4_ROWS;
   int pages = 0;
-  if (lane < p.c.B) pages = (min(min(max(p.n_ctx[lane], 0), max(cap - p.n_local, 0)) + p.n_local, cap) + KV4_ROWS - 1) / KV4_ROWS;
+  bool inside;
+  if (lane < p.c.B) pages = (rows_of(p, lane, inside).total + KV4_ROWS - 1) / KV4_ROWS;
   const int total = __reduce_add_sync(0xffffffffu, pages);
   // lane c tries the c-th size of a part; the smallest with slots enough for all is taken (or one part each)
   const float size = fmaxf(static_cast<float>(total) / p.slots, static_cast<float>(p.least_pages)) * (1.f + lane / 16.f + lane * lane / 64.f);

@@ -6,7 +6,8 @@ import pytest
 import torch
 
 import paper_2402_15758_gb300 as pkg
-from test_gpu_ops4 import ATT_TOL, BF16_TOL, Cache, _anc, _gen, _ints, _masks, _normal, _probabilities, _rel_rows, _stands_for
+from test_gpu_ops4 import (ATT_TOL, BF16_TOL, ECAPACITY, Cache, _anc, _gen, _ints, _masks, _normal, _probabilities, _rel_rows,
+                           _stands_for, _status)
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -180,3 +181,27 @@ def test_rows_of_equal_values_among_others(form, nq, size):
     pkg.op_kv4_append(cache.k[0].float().reshape(200, -1), torch.zeros(200, G * hd, device="cuda"), cache.pool, cache.table, _ints([0]),
                       200, hd)
     assert (_attend(cache, q, [200], [0] * nq, nq, 0, H, form)[0] == 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [2 ** 31 - 1, 2 ** 31 - 3, -2 ** 31, None])
+@pytest.mark.parametrize("batch", [1, 12])
+def test_lengths_past_the_table_are_reported(n, batch):
+    # n + n_local passes 32 bits, or the table by one slot (None); the other sequences of a (dealt) batch are as they were
+    G, hd, n_local = 16, 64, 4
+    g = _gen(61, batch)
+    cache = Cache(g, [29] + [500] * (batch - 1), G, hd, pages=3 if batch == 1 else 40)
+    slots = cache.pages * 16
+    ctx = [25] + [496] * (batch - 1)
+    masks = _masks("chain", n_local, None)
+    q = _normal(g, batch * n_local, G * hd)
+    ref, _ = _reference(cache, q, ctx, masks, n_local, n_local, G)
+    lengths = _ints([slots - n_local + 1 if n is None else n] + ctx[1:])
+    out, lse = torch.zeros(batch * n_local, G * hd, device="cuda"), torch.zeros(batch * n_local, G, device="cuda")
+    pkg.op_attention_kv4(q, cache.pool, cache.table, lengths, _anc(masks), out, n_local, 0, n_local, n_local, G, hd, lse=lse)
+    assert _status(pkg.op_sync) == ECAPACITY
+    if batch > 1:
+        assert _rel_rows(out.view(batch, n_local, G, hd)[1:], ref[1:]) <= ATT_TOL
+    scores = torch.zeros(batch, G, slots, device="cuda")
+    pkg.op_kv4_score(q, lse, cache.pool, cache.table, lengths, _anc(masks), scores, n_local, 0, n_local, n_local, G, hd)
+    assert _status(pkg.op_sync) == ECAPACITY
