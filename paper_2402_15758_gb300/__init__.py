@@ -16,6 +16,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libchimera.so")
 HEADER = os.path.join(os.path.dirname(_PKG), "include", "chimera.h")
 
+EINVAL = -1
 STATUS = {0: "OK", -1: "EINVAL", -2: "ENOMEM", -3: "ECAPACITY", -4: "ECUDA", -5: "ETIMEDOUT", -6: "ESTATE"}
 
 DBG = dict(node_tokens=1, verify_logits=2, verify_hidden=3, argmax=4, path=5, accept_len=6,
@@ -55,6 +56,10 @@ class Weights(ctypes.Structure):
 
 
 _lib = None
+# torch's types, known once the library is loaded; values go by their code in the library's calls
+_F32 = _BF16 = _U8 = _I32 = None
+_CODE: dict = {}
+_MASKS: frozenset = frozenset()
 
 _KV4_ROWS = [ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_int,
              ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
@@ -117,7 +122,7 @@ _SIGS = {
 
 def load(path: str = LIB_PATH):
     """Load the library (built by build.py / __graft_entry__.build); raises if absent."""
-    global _lib
+    global _lib, _F32, _BF16, _U8, _I32, _CODE, _MASKS
     if _lib is not None:
         return _lib
     if not os.path.exists(path):
@@ -128,6 +133,9 @@ def load(path: str = LIB_PATH):
         fn = getattr(lib, name)
         fn.restype = res
         fn.argtypes = args
+    import torch
+    _F32, _BF16, _U8, _I32 = torch.float32, torch.bfloat16, torch.uint8, torch.int32
+    _CODE, _MASKS = {_F32: 0, _BF16: 1}, frozenset((torch.int64, torch.uint64))
     _lib = lib
     return lib
 
@@ -415,71 +423,112 @@ def w4_round(w, group: int = 128):
     return (code[:, 0::2] | code[:, 1::2] << 4).contiguous(), scale, zero.to(torch.uint8)
 
 
-def _code(t) -> int:
-    return 0 if t.element_size() == 4 else 1
+# The checks stand inside the calls, one expression each: of a call's 5 to 9 us on the host a function per tensor
+# would take two.
+def _refused(call: str) -> ChimeraError:
+    return ChimeraError(EINVAL, f"{call}: the type or the strides of a tensor")
 
 
 def op_linear_w4(X, W, scales, Y, zeros=None, group: int = 128, epi: int = 0, out_f32: bool = False, X_lo=None, stream=None):
-    """Y (epilogue)= (X + X_lo) W^T with 4-bit weights through chimera_op_linear_w4: X, X_lo [M][K] (bf16; X fp32
-    without X_lo), W uint8 [N][K / 2], scales bf16 and zeros uint8 (or None: 8) [N][ceil(K / group)]."""
-    M, K = X.shape
-    st = load().chimera_op_linear_w4(_code(X), epi, int(out_f32), M, W.shape[0], K, group, _ptr(X), _ptr(X_lo), X.stride(0),
-                                     _ptr(W), _ptr(scales), _ptr(zeros), _ptr(Y), Y.stride(0), _stream_handle(stream))
+    """Y (epilogue)= (X + X_lo) W^T with 4-bit weights through chimera_op_linear_w4: X, X_lo [M][K] (bf16, of one row
+    stride; or X fp32 without X_lo), W uint8 [N][K / 2], scales bf16 and zeros uint8 (or None: 8) [N][ceil(K / group)],
+    Y [M][N] fp32 where X is, with epi 2 and with out_f32, bf16 otherwise."""
+    lib = _lib or load()
+    code, (M, K), N, (ldx, x1), (ldy, y1) = _CODE.get(X.dtype), X.shape, W.shape[0], X.stride(), Y.stride()
+    if (code is None or x1 != 1 or W.dtype is not _U8 or not W.is_contiguous() or scales.dtype is not _BF16 or
+            not scales.is_contiguous() or Y.dtype is not (_F32 if code == 0 or epi == 2 or out_f32 else _BF16) or
+            (y1 != 1 and N != 1) or (zeros is not None and (zeros.dtype is not _U8 or not zeros.is_contiguous())) or
+            (X_lo is not None and (X_lo.dtype is not _BF16 or X_lo.stride() != (ldx, 1)))):
+        raise _refused("chimera_op_linear_w4")
+    st = lib.chimera_op_linear_w4(code, epi, int(out_f32), M, N, K, group, X.data_ptr(), _ptr(X_lo), ldx, W.data_ptr(),
+                                  scales.data_ptr(), _ptr(zeros), Y.data_ptr(), ldy, _stream_handle(stream))
     if st != 0:
         raise ChimeraError(st, "chimera_op_linear_w4")
 
 
+def _kv4_rows(fn, k, v, pool, page_table, slot0, rows, head_dim, counts, stream):
+    code, (ldk, k1), (ldv, v1) = _CODE.get(k.dtype), k.stride(), v.stride()
+    (batch, max_pages), (blocks, kv_heads, _) = page_table.shape, pool.shape
+    if (code is None or v.dtype is not k.dtype or k1 != 1 or v1 != 1 or pool.dtype is not _U8 or not pool.is_contiguous() or
+            page_table.dtype is not _I32 or not page_table.is_contiguous() or slot0.dtype is not _I32 or
+            not slot0.is_contiguous() or (counts is not None and (counts.dtype is not _I32 or not counts.is_contiguous()))):
+        raise _refused(fn.__name__)
+    st = fn(code, batch, rows, kv_heads, head_dim, k.data_ptr(), ldk, v.data_ptr(), ldv, pool.data_ptr(), blocks,
+            page_table.data_ptr(), max_pages, slot0.data_ptr(), _ptr(counts), _stream_handle(stream))
+    if st != 0:
+        raise ChimeraError(st, fn.__name__)
+
+
 def op_kv4_append(k, v, pool, page_table, slot0, rows, head_dim, counts=None, stream=None):
     """Round K and V rows to 4 bits into slots slot0[b] + i of each sequence, i < rows (or counts[b]), through
-    chimera_op_kv4_append.  k, v [batch * rows][kv_heads * head_dim] fp32 or bf16; pool from kv4_pool; page_table int32
-    [batch][max_pages]; slot0, counts int32 [batch] on the device."""
-    st = load().chimera_op_kv4_append(_code(k), page_table.shape[0], rows, pool.shape[1], head_dim, _ptr(k), k.stride(0),
-                                      _ptr(v), v.stride(0), _ptr(pool), pool.shape[0], _ptr(page_table),
-                                      page_table.shape[1], _ptr(slot0), _ptr(counts), _stream_handle(stream))
-    if st != 0:
-        raise ChimeraError(st, "chimera_op_kv4_append")
+    chimera_op_kv4_append.  k, v [batch * rows][kv_heads * head_dim] both fp32 or both bf16; pool from kv4_pool; page_table
+    int32 [batch][max_pages]; slot0, counts int32 [batch] on the device."""
+    _kv4_rows((_lib or load()).chimera_op_kv4_append, k, v, pool, page_table, slot0, rows, head_dim, counts, stream)
 
 
 def op_kv4_read(pool, page_table, slot0, rows, head_dim, k, v, counts=None, stream=None):
     """What the cached rows stand for, into k and v (shapes as in op_kv4_append), through chimera_op_kv4_read."""
-    st = load().chimera_op_kv4_read(_code(k), page_table.shape[0], rows, pool.shape[1], head_dim, _ptr(k), k.stride(0),
-                                    _ptr(v), v.stride(0), _ptr(pool), pool.shape[0], _ptr(page_table), page_table.shape[1],
-                                    _ptr(slot0), _ptr(counts), _stream_handle(stream))
-    if st != 0:
-        raise ChimeraError(st, "chimera_op_kv4_read")
+    _kv4_rows((_lib or load()).chimera_op_kv4_read, k, v, pool, page_table, slot0, rows, head_dim, counts, stream)
 
 
 def op_attention_kv4(q, pool, page_table, n_ctx, anc, out, nq, q_local0, n_local, q_rows, n_heads, head_dim, out_lo=None,
                      lse=None, splits=0, stream=None):
     """Tree-masked attention over the 4-bit cache through chimera_op_attention_kv4: op_attention's rows and masks,
-    q fp32 or bf16, out fp32 or bf16 (+ out_lo), lse fp32 [batch * q_rows][n_heads] (optional)."""
-    st = load().chimera_op_attention_kv4(_code(q), _code(out), n_ctx.shape[0], n_heads, pool.shape[1], head_dim, nq, q_local0,
-                                         n_local, _ptr(q), q.stride(0), q_rows, _ptr(pool), pool.shape[0],
-                                         _ptr(page_table), page_table.shape[1], _ptr(n_ctx), _ptr(anc), _ptr(out),
-                                         _ptr(out_lo), out.stride(0), _ptr(lse), splits, _stream_handle(stream))
+    q fp32 or bf16, out fp32 or bf16 (+ out_lo of the same row stride), lse fp32 [batch * q_rows][n_heads] (optional)."""
+    lib = _lib or load()
+    q_code, out_code, (ldq, q1), (ldo, o1) = _CODE.get(q.dtype), _CODE.get(out.dtype), q.stride(), out.stride()
+    blocks, kv_heads, _ = pool.shape
+    if (q_code is None or out_code is None or q1 != 1 or o1 != 1 or pool.dtype is not _U8 or not pool.is_contiguous() or
+            page_table.dtype is not _I32 or not page_table.is_contiguous() or n_ctx.dtype is not _I32 or
+            not n_ctx.is_contiguous() or (anc is not None and (anc.dtype not in _MASKS or not anc.is_contiguous())) or
+            (lse is not None and (lse.dtype is not _F32 or not lse.is_contiguous())) or
+            (out_lo is not None and (out_lo.dtype is not _BF16 or out_lo.stride() != (ldo, 1)))):
+        raise _refused("chimera_op_attention_kv4")
+    st = lib.chimera_op_attention_kv4(q_code, out_code, n_ctx.shape[0], n_heads, kv_heads, head_dim, nq, q_local0, n_local,
+                                      q.data_ptr(), ldq, q_rows, pool.data_ptr(), blocks, page_table.data_ptr(),
+                                      page_table.shape[1], n_ctx.data_ptr(), _ptr(anc), out.data_ptr(), _ptr(out_lo), ldo,
+                                      _ptr(lse), splits, _stream_handle(stream))
     if st != 0:
         raise ChimeraError(st, "chimera_op_attention_kv4")
 
 
 def op_kv4_score(q, lse, pool, page_table, n_ctx, anc, scores, nq, q_local0, n_local, q_rows, n_heads, head_dim, weight=None,
                  stream=None):
-    """Add the attention weight that each cached row draws to scores (fp32 [batch][kv_heads][slots]) through
-    chimera_op_kv4_score; lse from op_attention_kv4, weight fp32 [batch * q_rows] or None."""
-    st = load().chimera_op_kv4_score(_code(q), n_ctx.shape[0], n_heads, pool.shape[1], head_dim, nq, q_local0, n_local, _ptr(q),
-                                     q.stride(0), q_rows, _ptr(lse), _ptr(weight), _ptr(pool), pool.shape[0],
-                                     _ptr(page_table), page_table.shape[1], _ptr(n_ctx), _ptr(anc), _ptr(scores),
-                                     scores.stride(1), _stream_handle(stream))
+    """Add the attention weight that each cached row draws to scores (fp32 [batch][kv_heads][slots], all heads the same
+    distance apart) through chimera_op_kv4_score; lse from op_attention_kv4, weight fp32 [batch * q_rows] or None."""
+    lib = _lib or load()
+    q_code, (ldq, q1), (ldb, lds, s1), batch, (blocks, kv_heads, _) = (_CODE.get(q.dtype), q.stride(), scores.stride(),
+                                                                       n_ctx.shape[0], pool.shape)
+    if (q_code is None or q1 != 1 or lse.dtype is not _F32 or not lse.is_contiguous() or scores.dtype is not _F32 or s1 != 1 or
+            (ldb != kv_heads * lds and batch != 1) or pool.dtype is not _U8 or not pool.is_contiguous() or
+            page_table.dtype is not _I32 or not page_table.is_contiguous() or n_ctx.dtype is not _I32 or
+            not n_ctx.is_contiguous() or (anc is not None and (anc.dtype not in _MASKS or not anc.is_contiguous())) or
+            (weight is not None and (weight.dtype is not _F32 or not weight.is_contiguous()))):
+        raise _refused("chimera_op_kv4_score")
+    st = lib.chimera_op_kv4_score(q_code, batch, n_heads, kv_heads, head_dim, nq, q_local0, n_local, q.data_ptr(), ldq, q_rows,
+                                  lse.data_ptr(), _ptr(weight), pool.data_ptr(), blocks, page_table.data_ptr(),
+                                  page_table.shape[1], n_ctx.data_ptr(), _ptr(anc), scores.data_ptr(), lds, _stream_handle(stream))
     if st != 0:
         raise ChimeraError(st, "chimera_op_kv4_score")
 
 
 def op_kv4_evict(pool, page_table, n_ctx, scores, budget, recent, dst_table, kept, scores_out, n_out, head_dim, stream=None):
     """Keep the `recent` newest rows and the best-scored of the others, `budget` in all, per head, in the pages of
-    dst_table, through chimera_op_kv4_evict (kept int32 and scores_out fp32 [batch][kv_heads][budget], n_out int32 [batch])."""
-    st = load().chimera_op_kv4_evict(n_ctx.shape[0], pool.shape[1], head_dim, _ptr(pool), pool.shape[0], _ptr(page_table),
-                                     page_table.shape[1], _ptr(n_ctx), _ptr(scores), scores.stride(1), budget, recent,
-                                     _ptr(dst_table), dst_table.shape[1], _ptr(kept), _ptr(scores_out), _ptr(n_out),
-                                     _stream_handle(stream))
+    dst_table, through chimera_op_kv4_evict (scores as in op_kv4_score; kept int32 and scores_out fp32
+    [batch][kv_heads][budget], n_out int32 [batch])."""
+    lib = _lib or load()
+    (ldb, lds, s1), batch, (blocks, kv_heads, _) = scores.stride(), n_ctx.shape[0], pool.shape
+    if (scores.dtype is not _F32 or s1 != 1 or (ldb != kv_heads * lds and batch != 1) or pool.dtype is not _U8 or
+            not pool.is_contiguous() or page_table.dtype is not _I32 or not page_table.is_contiguous() or
+            n_ctx.dtype is not _I32 or not n_ctx.is_contiguous() or dst_table.dtype is not _I32 or
+            not dst_table.is_contiguous() or kept.dtype is not _I32 or not kept.is_contiguous() or
+            scores_out.dtype is not _F32 or not scores_out.is_contiguous() or n_out.dtype is not _I32 or
+            not n_out.is_contiguous()):
+        raise _refused("chimera_op_kv4_evict")
+    st = lib.chimera_op_kv4_evict(batch, kv_heads, head_dim, pool.data_ptr(), blocks, page_table.data_ptr(), page_table.shape[1],
+                                  n_ctx.data_ptr(), scores.data_ptr(), lds, budget, recent, dst_table.data_ptr(),
+                                  dst_table.shape[1], kept.data_ptr(), scores_out.data_ptr(), n_out.data_ptr(),
+                                  _stream_handle(stream))
     if st != 0:
         raise ChimeraError(st, "chimera_op_kv4_evict")
 

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2402_15758_gb300 as pkg
-from test_gpu_ops4 import (ATT_TOL, BF16_TOL, ECAPACITY, Cache, _anc, _gen, _ints, _masks, _normal, _probabilities, _rel_rows,
+from test_gpu_ops4 import (ATT_TOL, BF16_TOL, ECAPACITY, EINVAL, Cache, _anc, _gen, _ints, _masks, _normal, _probabilities, _rel_rows,
                            _stands_for, _status)
 
 
@@ -205,3 +205,62 @@ def test_lengths_past_the_table_are_reported(n, batch):
     scores = torch.zeros(batch, G, slots, device="cuda")
     pkg.op_kv4_score(q, lse, cache.pool, cache.table, lengths, _anc(masks), scores, n_local, 0, n_local, n_local, G, hd)
     assert _status(pkg.op_sync) == ECAPACITY
+
+
+def test_tensors_of_other_types_and_strides_are_refused():
+    """Before the library is called: each of these would be read or written as something that it is not."""
+    f32, bf16, f16, f64, u8, i32, i64 = (torch.float32, torch.bfloat16, torch.float16, torch.float64, torch.uint8, torch.int32,
+                                         torch.int64)
+    z = torch.zeros
+
+    def linear(**kw):
+        d = dict(X=z(4, 64, dtype=bf16), W=z(8, 32, dtype=u8), scales=z(8, 1, dtype=bf16), Y=z(4, 8, dtype=bf16), zeros=z(8, 1, dtype=u8),
+                 group=64)
+        d.update(kw)
+        return pkg.op_linear_w4, d
+
+    def rows(fn=pkg.op_kv4_append, **kw):
+        d = dict(k=z(3, 128), v=z(3, 128), pool=z(1, 1, 16 * 128 + 128, dtype=u8), page_table=z(1, 1, dtype=i32), slot0=z(1, dtype=i32),
+                 rows=3, head_dim=128)
+        d.update(kw)
+        return fn, d
+
+    def queries(fn, **kw):
+        d = dict(q=z(2, 256), pool=z(1, 2, 16 * 128 + 128, dtype=u8), page_table=z(1, 1, dtype=i32), n_ctx=z(1, dtype=i32),
+                 anc=z(2, dtype=i64), lse=z(2, 2), nq=2, q_local0=0, n_local=2, q_rows=2, n_heads=2, head_dim=128)
+        d.update(dict(out=z(2, 256)) if fn is pkg.op_attention_kv4 else dict(scores=z(1, 2, 16)))
+        d.update(kw)
+        return fn, d
+
+    def evict(**kw):
+        d = dict(pool=z(2, 2, 16 * 128 + 128, dtype=u8), page_table=z(2, 1, dtype=i32), n_ctx=z(2, dtype=i32), scores=z(2, 2, 16), budget=8,
+                 recent=2, dst_table=z(2, 1, dtype=i32), kept=z(2, 2, 8, dtype=i32), scores_out=z(2, 2, 8), n_out=z(2, dtype=i32),
+                 head_dim=128)
+        d.update(kw)
+        return pkg.op_kv4_evict, d
+
+    wide = z(4, 300, dtype=bf16)
+    bad = [linear(X=z(4, 64, dtype=f16)), linear(X=z(4, 64, dtype=f64)), linear(X=z(64, 4, dtype=bf16).t()), linear(Y=z(4, 8)),
+           linear(Y=z(4, 8, dtype=f16)), linear(out_f32=True), linear(epi=2), linear(X=z(4, 64)), linear(Y=z(8, 4, dtype=bf16).t()),
+           linear(W=z(8, 32, dtype=f32)), linear(W=z(32, 8, dtype=u8).t()), linear(scales=z(8, 1)), linear(scales=z(8, 1, dtype=f16)),
+           linear(zeros=z(8, 1, dtype=i32)), linear(X_lo=z(4, 64)), linear(X_lo=wide[:, :64])]
+    for fn in (pkg.op_kv4_append, pkg.op_kv4_read):
+        bad += [rows(fn, k=z(3, 128, dtype=f16), v=z(3, 128, dtype=f16)), rows(fn, k=z(3, 128, dtype=f64), v=z(3, 128, dtype=f64)),
+                rows(fn, v=z(3, 128, dtype=bf16)), rows(fn, k=z(3, 128, dtype=bf16)), rows(fn, k=z(128, 3).t()),
+                rows(fn, v=z(3, 256)[:, ::2]), rows(fn, page_table=z(1, 1, dtype=i64)), rows(fn, page_table=z(2, 2, dtype=i32)[:, :1]), rows(fn, slot0=z(1, dtype=i64)),
+                rows(fn, counts=z(1, dtype=i64)), rows(fn, pool=z(1, 1, 16 * 128 + 128, dtype=f32))]
+    for fn in (pkg.op_attention_kv4, pkg.op_kv4_score):
+        bad += [queries(fn, q=z(2, 256, dtype=f16)), queries(fn, q=z(2, 256, dtype=f64)), queries(fn, q=z(256, 2).t()),
+                queries(fn, lse=z(2, 2, dtype=bf16)), queries(fn, lse=z(2, 4)[:, ::2]), queries(fn, anc=z(2, dtype=i32)),
+                queries(fn, n_ctx=z(1, dtype=i64)), queries(fn, page_table=z(1, 1, dtype=i64)),
+                queries(fn, pool=z(1, 2, 16 * 128 + 128, dtype=i32))]
+    bad += [queries(pkg.op_attention_kv4, out=z(2, 256, dtype=f16)), queries(pkg.op_attention_kv4, out=z(256, 2).t()),
+            queries(pkg.op_attention_kv4, out=z(2, 256, dtype=bf16), out_lo=z(2, 256)),
+            queries(pkg.op_attention_kv4, out=z(2, 256, dtype=bf16), out_lo=wide[:2, :256])]
+    two = dict(q=z(4, 256), n_ctx=z(2, dtype=i32), page_table=z(2, 1, dtype=i32), lse=z(4, 2))
+    bad += [queries(pkg.op_kv4_score, scores=z(1, 2, 16, dtype=f64)), queries(pkg.op_kv4_score, scores=z(1, 2, 32)[:, :, ::2]),
+            queries(pkg.op_kv4_score, scores=z(2, 3, 16)[:, 1:], **two), queries(pkg.op_kv4_score, weight=z(2, dtype=f64)),
+            evict(scores=z(2, 3, 16)[:, :2]), evict(scores=z(2, 2, 16, dtype=bf16)), evict(kept=z(2, 2, 8, dtype=i64)),
+            evict(scores_out=z(2, 2, 8, dtype=bf16)), evict(n_out=z(2, dtype=i64)), evict(dst_table=z(2, 1, dtype=i64))]
+    for fn, d in bad:
+        assert _status(fn, **d) == EINVAL, (fn.__name__, {k: (v.dtype, v.stride()) if hasattr(v, "dtype") else v for k, v in d.items()})
