@@ -320,8 +320,8 @@ chimera_status chimera_op_attention(int dtype, int kv_split, int batch, int n_he
 /* ---- 4-bit serving: weights and KV cache in 4 bits (stateless, like the ones above) ----
  * The paper keeps weights and caches in 16 bits; these operators are a service of the
  * library for serving the same models from a quarter of the bytes.  All are asynchronous on
- * `cuda_stream` (NULL: default), take device pointers, and may overlap on several streams under
- * chimera_op_linear's rule.  What a kernel meets on the device (a slot past the table: ECAPACITY;
+ * `cuda_stream` (NULL: default), take device pointers aligned to their elements (more where it says so), and may overlap
+ * on several streams under chimera_op_linear's rule.  What a kernel meets on the device (a slot past the table: ECAPACITY;
  * a block past the pool: EINVAL; such rows are skipped) is reported by chimera_op_sync.
  *
  * Y[M][N] (epilogue)= (X + X_lo)[M][K] . W^T with W[n][k] = scale[n][k / group] *

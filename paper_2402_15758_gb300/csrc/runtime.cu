@@ -6,6 +6,7 @@
 #include <cstdio>
 #include <cstring>
 #include <functional>
+#include <initializer_list>
 #include <mutex>
 #include <string>
 #include <utility>
@@ -2039,7 +2040,11 @@ OpScratch* op_scratch(cudaStream_t s) {
   if (!sh.ready && !op_alloc(&sh, true)) return nullptr;
   return cudaStreamWaitEvent(s, sh.done, 0) == cudaSuccess ? &sh : nullptr;
 }
-bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+bool aligned(int to, std::initializer_list<const void*> pointers) {  // null ones among them
+  for (const void* p : pointers)
+    if (reinterpret_cast<uintptr_t>(p) % to != 0) return false;
+  return true;
+}
 const OpScratch kNoScratch;
 bool op_done(const OpScratch* sc, cudaStream_t s) { return !sc->done || cudaEventRecord(sc->done, s) == cudaSuccess; }
 }  // namespace
@@ -2116,11 +2121,10 @@ chimera_status chimera_op_linear_w4(int dtype, int epi, int out_f32, int M, int 
   const int wide = dtype == 0 ? 4 : 8;  // values in 16 bytes
   if ((dtype != 0 && dtype != 1) || epi < 0 || epi > 2 || M < 1 || N < 1 || K < 32 || K % 32 != 0 ||
       (group != 32 && group != 64 && group != 128) || !X || !W || !scales || !Y || ldx < K || ldx % wide != 0 || ldy < N ||
-      (dtype == 0 && X_lo) || M > 65535 * 8 || !aligned16(X) || !aligned16(X_lo) || !aligned16(W) ||
-      !aligned16(scales) || !aligned16(zeros))
+      (dtype == 0 && X_lo) || M > 65535 * 8 || !aligned(16, {X, X_lo, W, scales, zeros}))
     return CHIMERA_EINVAL;
   const int f32 = dtype == 0 || epi == EPI_RESID || out_f32;
-  if (reinterpret_cast<uintptr_t>(Y) % (f32 ? 4 : 2) != 0) return CHIMERA_EINVAL;
+  if (!aligned(f32 ? 4 : 2, {Y})) return CHIMERA_EINVAL;
   W4Params p{};
   p.X = X;
   p.X_lo = static_cast<const bf16_raw*>(X_lo);
@@ -2151,7 +2155,7 @@ chimera_status chimera_op_linear_w4(int dtype, int epi, int out_f32, int M, int 
 
 namespace {
 bool kv4_pool_ok(const void* pool, int n_blocks, const int32_t* table, int max_pages, int batch, int kv_heads, int head_dim) {
-  return pool && aligned16(pool) && n_blocks >= 1 && table && max_pages >= 1 && max_pages <= (1 << 26) && batch >= 1 &&
+  return pool && aligned(16, {pool}) && n_blocks >= 1 && table && aligned(4, {table}) && max_pages >= 1 && max_pages <= (1 << 26) && batch >= 1 &&
          batch <= 65535 && kv_heads >= 1 && kv_heads <= 65535 && batch * static_cast<long long>(kv_heads) <= 65535 &&
          (head_dim == 64 || head_dim == 128);
 }
@@ -2166,7 +2170,7 @@ chimera_status kv4_rows(bool append, int dtype, int batch, int rows, int kv_head
   const long long width = static_cast<long long>(kv_heads) * head_dim;
   if ((dtype != 0 && dtype != 1) || !kv4_pool_ok(pool, n_blocks, table, max_pages, batch, kv_heads, head_dim) || rows < 0 ||
       !k || !v || ldk < width || ldv < width || !slot0 || 2LL * batch * rows * kv_heads > (1LL << 33) ||
-      reinterpret_cast<uintptr_t>(k) % (dtype ? 2 : 4) != 0 || reinterpret_cast<uintptr_t>(v) % (dtype ? 2 : 4) != 0)
+      !aligned(dtype ? 2 : 4, {k, v}) || !aligned(4, {slot0, counts}))
     return CHIMERA_EINVAL;
   if (rows == 0) return CHIMERA_OK;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
@@ -2185,7 +2189,7 @@ bool kv4_queries(Kv4AttnParams* p, int dtype, int batch, int n_heads, int kv_hea
   if ((dtype != 0 && dtype != 1) || !kv4_pool_ok(pool, n_blocks, table, max_pages, batch, kv_heads, head_dim) ||
       n_heads < 1 || n_heads > 65535 || n_heads % kv_heads != 0 || nq < 1 || nq > 64 || n_local < 0 || n_local > 64 || q_local0 < 0 ||
       q_local0 > 63 || !q || ldq < n_heads * static_cast<long long>(head_dim) || q_rows < nq || !n_ctx || (n_local > 0 && !anc) ||
-      reinterpret_cast<uintptr_t>(q) % (dtype ? 2 : 4) != 0)
+      !aligned(dtype ? 2 : 4, {q}) || !aligned(4, {n_ctx}) || !aligned(8, {anc}))
     return false;
   p->q = q;
   p->q_f32 = dtype == 0;
@@ -2225,7 +2229,7 @@ chimera_status chimera_op_attention_kv4(int q_dtype, int out_dtype, int batch, i
   if (!kv4_queries(&p, q_dtype, batch, n_heads, kv_heads, head_dim, nq, q_local0, n_local, q, ldq, q_rows, pool, n_blocks,
                    page_table, max_pages, n_ctx, anc) ||
       (out_dtype != 0 && out_dtype != 1) || !out || (out_dtype == 0 && out_lo) || ldo < n_heads * head_dim || splits < 0 ||
-      splits > 64 || reinterpret_cast<uintptr_t>(out) % (out_dtype ? 2 : 4) != 0)
+      splits > 64 || !aligned(out_dtype ? 2 : 4, {out, out_lo}) || !aligned(4, {lse}))
     return CHIMERA_EINVAL;
   p.c = kv4_pool(pool, n_blocks, page_table, max_pages, batch, kv_heads, head_dim, &kNoScratch);
   p.out = out;
@@ -2253,7 +2257,7 @@ chimera_status chimera_op_kv4_score(int q_dtype, int batch, int n_heads, int kv_
   Kv4AttnParams p{};
   if (!kv4_queries(&p, q_dtype, batch, n_heads, kv_heads, head_dim, nq, q_local0, n_local, q, ldq, q_rows, pool, n_blocks,
                    page_table, max_pages, n_ctx, anc) ||
-      !lse || !scores || ld_scores < 1)
+      !lse || !scores || ld_scores < 1 || !aligned(4, {lse, weight, scores}))
     return CHIMERA_EINVAL;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   std::lock_guard<std::mutex> lk(g_op_mu);
@@ -2274,7 +2278,7 @@ chimera_status chimera_op_kv4_evict(int batch, int kv_heads, int head_dim, void*
                                     int32_t* n_out, void* cuda_stream) {
   if (!kv4_pool_ok(pool, n_blocks, page_table, max_pages, batch, kv_heads, head_dim) || !n_ctx || !scores || ld_scores < 1 ||
       budget < 1 || recent < 0 || recent > budget || !dst_table || dst_pages < 1 || (budget + 15) / 16 > dst_pages || !kept ||
-      !scores_out || !n_out)
+      !scores_out || !n_out || !aligned(4, {n_ctx, scores, dst_table, kept, scores_out, n_out}))
     return CHIMERA_EINVAL;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   std::lock_guard<std::mutex> lk(g_op_mu);

@@ -247,8 +247,8 @@ def test_tensors_of_other_types_and_strides_are_refused():
     for fn in (pkg.op_kv4_append, pkg.op_kv4_read):
         bad += [rows(fn, k=z(3, 128, dtype=f16), v=z(3, 128, dtype=f16)), rows(fn, k=z(3, 128, dtype=f64), v=z(3, 128, dtype=f64)),
                 rows(fn, v=z(3, 128, dtype=bf16)), rows(fn, k=z(3, 128, dtype=bf16)), rows(fn, k=z(128, 3).t()),
-                rows(fn, v=z(3, 256)[:, ::2]), rows(fn, page_table=z(1, 1, dtype=i64)), rows(fn, page_table=z(2, 2, dtype=i32)[:, :1]), rows(fn, slot0=z(1, dtype=i64)),
-                rows(fn, counts=z(1, dtype=i64)), rows(fn, pool=z(1, 1, 16 * 128 + 128, dtype=f32))]
+                rows(fn, v=z(3, 256)[:, ::2]), rows(fn, page_table=z(1, 1, dtype=i64)), rows(fn, page_table=z(2, 2, dtype=i32)[:, :1]),
+                rows(fn, slot0=z(1, dtype=i64)), rows(fn, counts=z(1, dtype=i64)), rows(fn, pool=z(1, 1, 16 * 128 + 128, dtype=f32))]
     for fn in (pkg.op_attention_kv4, pkg.op_kv4_score):
         bad += [queries(fn, q=z(2, 256, dtype=f16)), queries(fn, q=z(2, 256, dtype=f64)), queries(fn, q=z(256, 2).t()),
                 queries(fn, lse=z(2, 2, dtype=bf16)), queries(fn, lse=z(2, 4)[:, ::2]), queries(fn, anc=z(2, dtype=i32)),
@@ -264,3 +264,27 @@ def test_tensors_of_other_types_and_strides_are_refused():
             evict(scores_out=z(2, 2, 8, dtype=bf16)), evict(n_out=z(2, dtype=i64)), evict(dst_table=z(2, 1, dtype=i64))]
     for fn, d in bad:
         assert _status(fn, **d) == EINVAL, (fn.__name__, {k: (v.dtype, v.stride()) if hasattr(v, "dtype") else v for k, v in d.items()})
+
+
+def _calls():
+    """The C entry points with arguments that they take; addresses are numbers that nothing reads."""
+    lib, a = pkg.load(), 4096
+    rows = dict(dtype=0, batch=1, rows=1, G=1, hd=128, k=a, ldk=128, v=a, ldv=128, pool=a, blocks=1, table=a, pages=1, slot0=a, counts=a)
+    cache = dict(pool=a, blocks=1, table=a, pages=1, n_ctx=a)
+    attention = dict(qd=1, od=1, batch=1, H=4, G=2, hd=128, nq=1, ql0=0, n_local=1, q=a, ldq=512, q_rows=1, **cache, anc=a, out=a, lo=a,
+                     ldo=512, lse=a, splits=0)
+    score = dict(qd=1, batch=1, H=4, G=2, hd=128, nq=1, ql0=0, n_local=1, q=a, ldq=512, q_rows=1, lse=a, weight=a, **cache, anc=a,
+                 scores=a, ld=16)
+    evict = dict(batch=1, G=1, hd=64, **cache, scores=a, ld=32, budget=16, recent=4, dst=a, dst_pages=1, kept=a, out=a, n_out=a)
+    return [(lib.chimera_op_kv4_append, rows), (lib.chimera_op_kv4_read, rows), (lib.chimera_op_attention_kv4, attention),
+            (lib.chimera_op_kv4_score, score), (lib.chimera_op_kv4_evict, evict)]
+
+
+def test_pointers_that_are_not_aligned_are_refused():
+    least = dict(k=4, v=4, pool=16, table=4, slot0=4, counts=4, n_ctx=4, q=2, anc=8, lo=2, lse=4, weight=4, scores=4, dst=4, kept=4,
+                 n_out=4)
+    for fn, args in _calls():
+        for name in args.keys() & (least.keys() | {"out"}):
+            step = least.get(name, 2 if "lo" in args else 4)
+            for off in {1, step // 2}:
+                assert fn(*{**args, name: args[name] + off}.values(), None) == EINVAL, (fn.__name__, name, off)
