@@ -1025,15 +1025,15 @@ Cut cut_of(const Kv4AttnParams& p) {
   const int rtw = rows <= nm * matrix ? 1 : rows <= 2 * nm * matrix || !precise ? 2 : 4;
   return Cut{precise, nm, rtw, nm * matrix * rtw};
 }
-int blocks_of(const Kv4AttnParams& p) {
-  const Cut c = cut_of(p);
-  return (p.nq * (p.H / p.c.G) + c.rows - 1) / c.rows * p.c.B * p.c.G;
-}
 }  // namespace
 
-int kv4_attn_blocks(const Kv4AttnParams& p) { return blocks_of(p); }
+long long kv4_attn_blocks(const Kv4AttnParams& p) {  // (any call's: more than 31 bits)
+  const Cut c = cut_of(p);
+  return static_cast<long long>((p.nq * (p.H / p.c.G) + c.rows - 1) / c.rows) * p.c.B * p.c.G;
+}
 
 namespace {
+int blocks_of(const Kv4AttnParams& p) { return static_cast<int>(kv4_attn_blocks(p)); }  // of a call that was taken
 // Blocks that are resident at once (launch bounds): three of one matrix in two terms (1 query over 16384 rows 30.6 us,
 // with two blocks 32.0; 8 of 256 to 4096 rows 40 and 56); otherwise two, without spills (4 queries of groups of 4
 // heads, bf16 out, 16384 rows: 17.5 us, with three 20.5), and two in clusters (1 query over 512 rows: 6.7, 7.3).

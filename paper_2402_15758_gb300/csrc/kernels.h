@@ -392,7 +392,7 @@ struct Kv4AttnParams {
   int ld_scores;
   const float* weight;  // optional [B * q_rows]
 };
-int kv4_attn_blocks(const Kv4AttnParams& p);  // of the grid, without its splits
+long long kv4_attn_blocks(const Kv4AttnParams& p);  // of the grid, without its splits
 void kv4_attn_split(Kv4AttnParams* p, int want, size_t most_floats);
 cudaError_t attention_kv4(const Kv4AttnParams& p, cudaStream_t s);
 cudaError_t kv4_score(const Kv4AttnParams& p, cudaStream_t s);

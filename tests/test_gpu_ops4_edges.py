@@ -288,3 +288,10 @@ def test_pointers_that_are_not_aligned_are_refused():
             step = least.get(name, 2 if "lo" in args else 4)
             for off in {1, step // 2}:
                 assert fn(*{**args, name: args[name] + off}.values(), None) == EINVAL, (fn.__name__, name, off)
+
+
+def test_a_grid_past_32_bits_is_refused():
+    fn, args = _calls()[2]
+    many = dict(batch=65535, H=65535, G=1, hd=64, nq=64, q_rows=64, ldq=65535 * 64, ldo=65535 * 64)
+    for more in (dict(), dict(lo=0, lse=0), dict(od=0, lo=0)):
+        assert fn(*{**args, **many, **more}.values(), None) == EINVAL
