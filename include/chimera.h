@@ -322,7 +322,8 @@ chimera_status chimera_op_attention(int dtype, int kv_split, int batch, int n_he
  * library for serving the same models from a quarter of the bytes.  All are asynchronous on
  * `cuda_stream` (NULL: default), take device pointers aligned to their elements (more where it says so), and may overlap
  * on several streams under chimera_op_linear's rule.  What a kernel meets on the device (a slot past the table: ECAPACITY;
- * a block past the pool: EINVAL; such rows are skipped) is reported by chimera_op_sync.
+ * a block past the pool: EINVAL) is reported by chimera_op_sync; append, read and eviction skip such rows, the attention
+ * and the weight sums of such a sequence are undefined.
  *
  * Y[M][N] (epilogue)= (X + X_lo)[M][K] . W^T with W[n][k] = scale[n][k / group] *
  * (code[n][k] - zero[n][k / group]).  W: uint8 [N][K / 2], the code of column 2 j in the low

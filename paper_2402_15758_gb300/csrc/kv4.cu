@@ -387,7 +387,7 @@ __global__ void __launch_bounds__(512, 4) kv4_move_kernel(Kv4EvictParams p) {
   using P = Kv4<HD>;
   const int bg = blockIdx.y, b = bg / p.c.G, g = bg % p.c.G, tid = threadIdx.x % 128, which = threadIdx.x / 128;
   const int page0 = blockIdx.x * MOVE_PAGES;
-  __shared__ const unsigned char* sh_src[MOVE_PAGES][KV4_ROWS];  // pages of the rows, null from the first that is not kept
+  __shared__ const unsigned char* sh_src[MOVE_PAGES][KV4_ROWS];  // pages of the rows; null: not kept, or no such block
   __shared__ int sh_row[MOVE_PAGES][KV4_ROWS];
   __shared__ unsigned char* sh_dst[MOVE_PAGES];
   if (threadIdx.x < MOVE_PAGES * KV4_ROWS) {
@@ -418,11 +418,11 @@ __global__ void __launch_bounds__(512, 4) kv4_move_kernel(Kv4EvictParams p) {
     if (!sh_dst[at]) continue;
     const unsigned char* s0 = first >= 0 ? sh_src[at][first] : nullptr;
     if (s0 && !is_v) x[j] = *reinterpret_cast<const uint4*>(s0 + sh_row[at][first] * P::ROW + k_at);
-    if (s0 && is_v) {
+    if (is_v) {
       const int r0 = sh_row[at][first], r1 = sh_row[at][first + 1];
       const unsigned char* s1 = sh_src[at][first + 1];
-      *reinterpret_cast<Chunk*>(x + j) = *reinterpret_cast<const Chunk*>(s0 + P::V + r0 / 2 * 2 * P::ROW + P::place(r0 / 2, chunk) * P::CHUNK);
-      y[j] = Chunk{};
+      *reinterpret_cast<Chunk*>(x + j) = y[j] = Chunk{};
+      if (s0) *reinterpret_cast<Chunk*>(x + j) = *reinterpret_cast<const Chunk*>(s0 + P::V + r0 / 2 * 2 * P::ROW + P::place(r0 / 2, chunk) * P::CHUNK);
       if (s1) y[j] = *reinterpret_cast<const Chunk*>(s1 + P::V + r1 / 2 * 2 * P::ROW + P::place(r1 / 2, chunk) * P::CHUNK);
     }
     if (tid < 2 * KV4_ROWS) {
@@ -435,7 +435,7 @@ __global__ void __launch_bounds__(512, 4) kv4_move_kernel(Kv4EvictParams p) {
     const int at = which * MOVE_ONCE + j;
     unsigned char* dst = sh_dst[at];
     if (!dst) continue;
-    const bool there = first >= 0 && sh_src[at][first];
+    const bool there = first >= 0 && (sh_src[at][first] || (is_v && sh_src[at][first + 1]));
     if (there && !is_v) *reinterpret_cast<uint4*>(dst + k_row * P::ROW + k_at) = x[j];
     if (there && is_v) {
       // halves of the words: row 2 pair from the half of its parity, row 2 pair + 1 likewise

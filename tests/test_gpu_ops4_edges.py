@@ -295,3 +295,28 @@ def test_a_grid_past_32_bits_is_refused():
     many = dict(batch=65535, H=65535, G=1, hd=64, nq=64, q_rows=64, ldq=65535 * 64, ldo=65535 * 64)
     for more in (dict(), dict(lo=0, lse=0), dict(od=0, lo=0)):
         assert fn(*{**args, **many, **more}.values(), None) == EINVAL
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hd", [64, 128])
+def test_eviction_skips_the_rows_of_a_bad_block_alone(hd):
+    G, n, budget = 2, 64, 47
+    g = _gen(71, hd)
+    cache = Cache(g, [n], G, hd, spare=3)
+    # kept of the older ones: slots 0 to 30 and 32 to 43, so that rows 30 and 31 of the result, a pair, are slots 30 and 32
+    scores = 1 + torch.rand(1, G, cache.pages * 16, generator=g, device="cuda")
+    scores[..., 31] = scores[..., 44:] = 0
+    table = cache.table.clone()
+    table[0, 1] = cache.pool.shape[0]  # slots 16 to 31
+    kept, out, n_out = torch.zeros(1, G, budget, dtype=torch.int32, device="cuda"), torch.zeros(1, G, budget, device="cuda"), _ints([0])
+    pkg.op_kv4_evict(cache.pool, table, _ints([n]), scores, budget, 4, cache.spare, kept, out, n_out, hd)
+    assert _status(pkg.op_sync) == EINVAL
+    k, v = torch.zeros(budget, G * hd, device="cuda"), torch.zeros(budget, G * hd, device="cuda")
+    pkg.op_kv4_read(cache.pool, cache.spare, _ints([0]), budget, hd, k, v)
+    pkg.op_sync()
+    for h in range(G):
+        at = kept[0, h].long()
+        good = (at < 16) | (at >= 32)
+        assert at[30:32].tolist() == [30, 32]
+        for got, want in ((k, cache.k), (v, cache.v)):
+            assert torch.equal(got.view(budget, G, hd)[good, h].double(), want[0, at[good], h].float().double())
