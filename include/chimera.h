@@ -341,8 +341,8 @@ chimera_status chimera_op_linear_w4(int dtype, int epi, int out_f32, int M, int 
  * head_dim 64 or 128; a page holds 16 rows (K and V) of one head, each as head_dim codes 0..15 and a
  * step and a base in bf16: base = bf16(min x), step = bf16((max x - min x) / 15; in fp32, times fp32(1 / 15)), code =
  * clamp(rint((x - base) / step), 0, 15), and the row stands for base + step * code.  A row of equal
- * values has step 0; a row holding a value that is not finite is kept as NaN.  page_table:
- * int32 [batch][max_pages], shared by all heads.
+ * values has step 0; a row holding a value that is not finite is kept as NaN, and so is one whose range is past fp32's or
+ * whose minimum is -inf in bf16.  page_table: int32 [batch][max_pages], shared by all heads.
  *
  * append rounds rows i < counts[b] (counts NULL: i < rows) of each sequence b into slots slot0[b] + i
  * (device int32 [batch]); k, v: [batch * rows][ld], head g at column g * head_dim, fp32

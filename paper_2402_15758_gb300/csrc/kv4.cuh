@@ -3,8 +3,8 @@
 // A row (one position of one kv head) of head_dim values is held as 4-bit codes with a step
 // and a base of its own, x = base + step * code:
 //   base = bf16(min x), step = bf16((max x - min x) fp32(1 / 15)), code = clamp(rint((x - base) / step), 0, 15)
-// (a row of equal values has step 0 and codes 0; a row with a value that is not finite is kept as
-// base NaN, step 0).  One step per row and head, not one per group of channels: then
+// (a row of equal values has step 0 and codes 0; a row with a value that is not finite, a range past
+// fp32's or a minimum past bf16's is kept as base NaN, step 0).  One step per row and head, not one per group of channels: then
 //   q . k      = step (q . code) + base (sum of q)
 //   sum p_j v_j = sum (p_j step_j) code_j + sum p_j base_j
 // and the codes enter the matrix products as whole numbers, exact in fp16, with no arithmetic

@@ -320,3 +320,39 @@ def test_eviction_skips_the_rows_of_a_bad_block_alone(hd):
         assert at[30:32].tolist() == [30, 32]
         for got, want in ((k, cache.k), (v, cache.v)):
             assert torch.equal(got.view(budget, G, hd)[good, h].double(), want[0, at[good], h].float().double())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_of_any_size_are_rounded_by_the_rule(hd, dtype):
+    # steps from subnormal numbers to 2^123 (the rounding scales those below 2^-60 and above 2^60)
+    sizes = [1e-41, 1e-38, 1e-30, 3e-19, 1e-18, 1.0, 1e18, 1e19, 3e19, 1e30, 1e36, 4e37]
+    g, n = _gen(67, hd), len(sizes)
+    rows = (_normal(g, n, 8, hd).clamp(-4, 4) * torch.tensor(sizes, device="cuda")[:, None, None]).view(-1, hd).to(dtype)
+    pages = rows.shape[0] // 16
+    pool, table, zero = pkg.kv4_pool(pages, 1, hd), torch.arange(pages, dtype=torch.int32, device="cuda").view(1, -1), _ints([0])
+    back = rows.flip(0).contiguous()
+    k, v = torch.zeros_like(rows), torch.zeros_like(rows)
+    pkg.op_kv4_append(rows, back, pool, table, zero, rows.shape[0], hd)
+    pkg.op_kv4_read(pool, table, zero, rows.shape[0], hd, k, v)
+    pkg.op_sync()
+    assert torch.equal(k, _stands_for(rows).float().to(dtype)) and torch.equal(v, _stands_for(back).float().to(dtype))
+
+
+@pytest.mark.gpu
+def test_rows_that_bf16_cannot_hold_are_no_numbers():
+    # a minimum that rounds to -inf in bf16, a range past fp32, and their neighbours
+    hd = 64
+    rows = torch.zeros(16, hd, device="cuda")
+    rows[0, 3] = -3.4e38
+    rows[1, 0], rows[1, 1] = 2e38, -2e38
+    rows[2, 0], rows[2, 1] = 1.5e38, -1.5e38
+    rows[3] = 3.38e38
+    pool, table, zero = pkg.kv4_pool(1, 1, hd), _ints([[0]]), _ints([0])
+    pkg.op_kv4_append(rows, rows, pool, table, zero, 16, hd)
+    k, v = torch.zeros_like(rows), torch.zeros_like(rows)
+    pkg.op_kv4_read(pool, table, zero, 16, hd, k, v)
+    pkg.op_sync()
+    for x in (k, v):
+        assert torch.isnan(x[:2]).all() and torch.equal(x[2:], _stands_for(rows[2:]).float())
