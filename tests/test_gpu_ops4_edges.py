@@ -7,7 +7,7 @@ import torch
 
 import paper_2402_15758_gb300 as pkg
 from test_gpu_ops4 import (ATT_TOL, BF16_TOL, ECAPACITY, EINVAL, Cache, _anc, _gen, _ints, _masks, _normal, _probabilities, _rel_rows,
-                           _stands_for, _status)
+                           _stands_for, _status, _weights)
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -356,3 +356,49 @@ def test_rows_that_bf16_cannot_hold_are_no_numbers():
     pkg.op_sync()
     for x in (k, v):
         assert torch.isnan(x[:2]).all() and torch.equal(x[2:], _stands_for(rows[2:]).float())
+
+
+# A rounding to bf16 is at most 2^-8 of the value.  Before it: sums of up to 128 codes of up to 15, with their zero or before
+# it is taken off, are cut toward zero at 2^-22 of what they have reached in each of up to 8 steps; of tokens that share
+# a sign that adds up over the groups, to 2^-15 of a row's largest result at worst (32 groups, codes around their zero).
+ROUNDED_TOL = 2.0 ** -8 + 2.0 ** -14
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K,group", [(1, 1000, 4096, 128), (3, 333, 4096, 64), (8, 250, 1056, 128), (5, 300, 4096, 32),
+                                         (40, 300, 4096, 128)])
+@pytest.mark.parametrize("kind", ["bf16", "split"])
+@pytest.mark.parametrize("zeros", [True, False])
+def test_linear_w4_rounded_results(M, N, K, group, kind, zeros):
+    g = _gen(73, M, N)
+    W, scale, zero, dense = _weights(g, N, K, group, zeros)
+    for mean in (0.0, 1.0, 30.0):  # activations around 0, and of one sign
+        x = _normal(g, M, K) + mean
+        hi = x.to(torch.bfloat16)
+        lo = (x - hi.float()).to(torch.bfloat16) if kind == "split" else None
+        ref = (hi.double() + (lo.double() if lo is not None else 0.0)) @ dense.T
+        Y = torch.full((M, N), float("nan"), dtype=torch.bfloat16, device="cuda")
+        pkg.op_linear_w4(hi, W, scale, Y, zeros=zero, group=group, X_lo=lo)
+        assert _rel_rows(Y, ref) <= ROUNDED_TOL
+    pkg.op_sync()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,group", [(5, 64), (5, 128), (8, 128), (40, 128)])
+@pytest.mark.parametrize("zeros", [True, False])
+def test_linear_w4_extreme_activations_rounded(M, group, zeros):
+    g = _gen(79, M)
+    W, scale, zero, dense = _weights(g, 300, 512, group, zeros)
+    x = _normal(g, M, 512).to(torch.bfloat16)
+    x[0, 7] = 3000.0  # one outlier
+    x[1] *= 1e30
+    x[2] *= 1e-30
+    x[3, 100] = float("inf")
+    x[4] = 0
+    Y = torch.full((M, 300), float("nan"), dtype=torch.bfloat16, device="cuda")
+    pkg.op_linear_w4(x, W, scale, Y, zeros=zero, group=group)
+    pkg.op_sync()
+    ref = x.double() @ dense.T
+    rest = [i for i in range(M) if i != 3]
+    assert _rel_rows(Y[rest], ref[rest]) <= ROUNDED_TOL
+    assert not torch.isfinite(Y[3]).all() and (Y[4] == 0).all()
