@@ -332,7 +332,7 @@ chimera_status chimera_op_attention(int dtype, int kv_split, int batch, int n_he
  * dtype 1: X, X_lo (optional) bf16; dtype 0: X fp32 (X_lo NULL), Y fp32.  X, X_lo and W
  * 16-byte aligned like the scales and zeros, ldx a multiple of 16 bytes.  epi and out_f32 as in chimera_op_linear.  Code less
  * zero is a whole number, so products are exact and are summed in fp32; a call's result
- * does not depend on timing (no sum is taken in arrival order). */
+ * does not depend on timing (no sum is taken in arrival order).  M at most 524280. */
 chimera_status chimera_op_linear_w4(int dtype, int epi, int out_f32, int M, int N, int K, int group, const void* X,
                                     const void* X_lo, int ldx, const void* W, const void* scales, const void* zeros,
                                     void* Y, int ldy, void* cuda_stream);
@@ -360,8 +360,11 @@ chimera_status chimera_op_kv4_read(int dtype, int batch, int rows, int kv_heads,
  * reads kv head h / (n_heads / kv_heads)).  q fp32 (q_dtype 0) or bf16 (1); out fp32 (out_dtype 0) or
  * bf16 (1) with an optional out_lo; lse (optional): fp32 [batch * q_rows][n_heads], natural log of each
  * row's sum of exponentials (-inf for a row that sees nothing, whose output is zero).  splits: as in
- * chimera_op_attention, at most 64; 0 lets the library choose.  A slot that no row may see
- * is never part of a result, whatever its page holds. */
+ * chimera_op_attention, at most 64; 0 lets the library choose (by max_pages and the batch, so a row's last bits may depend
+ * on them).  A slot is part of the results of the rows that may see it alone, whatever its page holds: a V row without
+ * numbers makes their outputs NaN (not their lse), and no others.  Weights of the softmax are held to 2^-22 of the row's
+ * largest; with a bf16 out, no out_lo, no lse and more than 8 rows per kv head (nq * n_heads / kv_heads) to 2^-12
+ * of their own, which asking for lse or out_lo changes. */
 chimera_status chimera_op_attention_kv4(int q_dtype, int out_dtype, int batch, int n_heads, int kv_heads, int head_dim, int nq,
                                         int q_local0, int n_local, const void* q, int ldq, int q_rows, const void* pool,
                                         int n_blocks, const int32_t* page_table, int max_pages, const int32_t* n_ctx,

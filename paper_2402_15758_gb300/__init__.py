@@ -1,4 +1,4 @@
-"""Thin Python binding of libchimera.so (argument marshalling only).
+"""Thin Python binding of libchimera.so (argument marshalling, and the tensors' types and strides where a call says so).
 
 Every step of the Chimera draft-and-verify path runs in the library's sm_103a
 kernels; this module only fills the C structs, passes device pointers (taken from

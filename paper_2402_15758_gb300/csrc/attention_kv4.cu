@@ -17,8 +17,10 @@
 //
 // Measured (GB300, hd 128, times of calls in a graph): 1 query of 32 heads over 512 rows 6.7 us (the launch, one trip to
 // memory after another, the join); over 16384 rows 30 us, 2.4 TB/s of 71 MB, bound by the instructions that turn codes
-// into numbers; 64 queries of 32 heads over 16384 rows 105 us (before the rows had units of their own 103: the tensor pipe was
-// active 47 % of the time and an instruction issued in 40 % two warps per scheduler, 250 registers each, wait for one another's results).
+// into numbers; 64 queries of 32 heads over 16384 rows 105 us, with weights in two terms 153: the tensor pipe is active
+// 45 % of the time (40 %) and an instruction issued in 41 % (48 %); two warps per scheduler, 250 registers each, wait for
+// one another's results.  The attention over a hi + lo cache in 16 bits takes 84 us for these 64 queries (540 MB); the 4-bit one
+// is the faster up to 16 queries: 30 us and 80 for 1, 41 to 45 and 81 for 16.
 #include <algorithm>
 
 #include "kernels.h"
@@ -828,9 +830,9 @@ struct ScoreSmem {
 
 // scores_j += sum over rows of weight p_j, p_j = 2^(z_j - lse): the first matrix product alone, on K's half of a page.
 // The fragments of up to 64 rows are held in shared memory, a page's codes are unpacked once for all of them.
-// Measured: 32 queries (24 that count) of 32 heads over 16384 rows (40 MB) 26.9 us, bound by the latency of products and
-// exponentials (tensor pipe 30 %, issue 50 %); two pages a time and eight warps a block, which halves the
-// fragments' way from shared memory, took 41.
+// Measured: 32 queries (24 that count) of 32 heads over 16384 rows (40 MB) 27.2 us, bound by the latency of products and
+// exponentials (tensor pipe 38 %, issue 45 %); two pages a time and eight warps a block, which halves the
+// fragments' way from shared memory, took 41 when one page took 33.
 template <int HD, typename TQ, bool DEAL>
 __global__ void __launch_bounds__(WARPS * 32) score_kv4_kernel(const __grid_constant__ Kv4AttnParams p) {
   extern __shared__ __align__(128) unsigned char smem[];
@@ -1012,7 +1014,7 @@ cudaError_t launch_sized(size_t smem, dim3 grid, const Kv4AttnParams& p, cudaStr
 // How a call's rows are cut: one term per weight where the result is rounded to bf16 alone and there are rows enough
 // to fill a matrix with them (32 heads over 16384 rows, 64 queries 105 us, with two terms 153; 16 queries 40.8 and
 // 45.2); two matrices per warp from there on, and warps that share pages for more rows (with one matrix and no
-// sharing: 143 and 287 us, 16 queries 41.9 and 51.7).
+// sharing 143 and 287 us where these took 102 and 146, 16 queries 41.9 and 51.7 for 41.8 and 43.7).
 namespace {
 struct Cut {
   bool precise;
@@ -1035,8 +1037,9 @@ long long kv4_attn_blocks(const Kv4AttnParams& p) {  // (any call's: more than 3
 namespace {
 int blocks_of(const Kv4AttnParams& p) { return static_cast<int>(kv4_attn_blocks(p)); }  // of a call that was taken
 // Blocks that are resident at once (launch bounds): three of one matrix in two terms (1 query over 16384 rows 30.6 us,
-// with two blocks 32.0; 8 of 256 to 4096 rows 40 and 56); otherwise two, without spills (4 queries of groups of 4
-// heads, bf16 out, 16384 rows: 17.5 us, with three 20.5), and two in clusters (1 query over 512 rows: 6.7, 7.3).
+// with two blocks 32.0; 8 of 256 to 4096 rows 40 and 56), although their 168 registers spill up to 76 bytes; otherwise two,
+// at 20 bytes at most (4 queries of groups of 4 heads, bf16 out, 16384 rows: 17.9 us, with three 20.5), and two in
+// clusters (1 query over 512 rows: 6.7, 7.3).
 int slots_of(const Cut& c) { return (c.nm == 1 && c.precise ? 3 : 2) * tc_num_sms(); }
 size_t ws_floats(const Kv4AttnParams& p) {
   const size_t parts = p.slots ? static_cast<size_t>(blocks_of(p)) / p.c.B * p.slots : static_cast<size_t>(blocks_of(p)) * p.splits;
@@ -1045,7 +1048,8 @@ size_t ws_floats(const Kv4AttnParams& p) {
 }  // namespace
 
 // The parts of the pages: `want` of every sequence, or (0) as many as are resident, none left for a second wave, dealt
-// to the sequences of a batch by their lengths.
+// to the sequences of a batch by their lengths.  The host knows the table's length, not the context's: with a table of four
+// times the context 1 query over 512 rows takes 7.6 us instead of 6.7 (no cluster), over 16384 rows 30.8 and 30.6.
 void kv4_attn_split(Kv4AttnParams* p, int want, size_t most_floats) {
   const Cut c = cut_of(*p);
   const int blocks = blocks_of(*p), at_once = WARPS / c.rtw * (c.nm == 1 ? 2 : 1);

@@ -60,7 +60,9 @@ __device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t b
   return r;
 }
 // The nibbles of a word as fp16 pairs (0,4), (1,5), (2,6), (3,7): 1024 + c in pairs 0 and 2, 1024 + 16 c in
-// 1 and 3 (ten bits of mantissa hold a nibble at either place).
+// 1 and 3 (ten bits of mantissa hold a nibble at either place).  The method, whole numbers put into the mantissa of a
+// power of two, is published in Kim, Henry, Fahim and Awadalla, "Who Says Elephants Can't Run: Bringing Large Scale
+// MoE Models into Cloud Scale Production" (2022).
 __device__ __forceinline__ void nibbles_f16(uint32_t w, uint32_t (&u)[4]) {
   const uint32_t h = w >> 8;
   u[0] = and_or(w, 0x000f000fu, 0x64006400u);

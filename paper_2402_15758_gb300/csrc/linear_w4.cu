@@ -29,10 +29,12 @@ constexpr int WARPS = 24, THREADS = WARPS * 32, FEATURES = 16;
 // codes without their zero are longer: the error is 2e-6 of the result instead of 2e-7, which fp32 results do without
 // (and sums of 32 cost more than they save: 23.1 us instead of 22.4).
 //
-// Measured (GB300, 22016 x 4096, group 128, 47 MB): one token 14.3 us, 3.3 TB/s, fp32 out 15.2, in two terms 17.8;
-// 8 tokens 19; 4096 x 4096 5.9 us.  Three CTAs of 8 warps, each with its own copy of the activations: 8 tokens 23 to 26,
-// 4096 x 4096 6.7.  Rings of bulk copies of 256 to 1024 bytes took 19.5 to 23, spans held in registers 17.7.  About
-// 4.5 us of every call are the launch, the activations and the join; the rest is bound by issue slots and the math pipe.
+// Measured (GB300, 22016 x 4096, group 128, 47 MB): one token 14.3 us, 3.3 TB/s, fp32 out 15.2, in two terms 17.8, group
+// 32 22.3; 8 tokens 19; 4096 x 4096 5.9 us (16-bit weights: one token 31.6, 8 tokens 32, 4096 x 4096 10.7).  Three CTAs of
+// 8 warps, each with its own copy of the activations: 8 tokens 23 to 26, 4096 x 4096 6.7.  Rings of bulk copies of 256 to 1024 bytes took 19.5 to 23, spans held in registers 17.7.  About
+// 4.5 us of every call are the launch, the activations and the join.  Over the whole launch an instruction is issued in
+// 51 % of the cycles, the ALUs are as busy, and the warps wait for a slot, the math pipe and shared memory in turn: no
+// single limit shows.  80 registers, of which groups of 128 spill 8 bytes.
 // From 9 tokens on, which would be a second column of matrices, the tensor cores' kernel: 22016 x 4096, 8 tokens 18.8 us
 // here, 22.0 there (1 token 14.3 and 21.9); 4096 x 4096 10.0 and 11.5; 8 tokens in two terms 23.9 in both.
 constexpr int FEW_TOKENS = 8;
@@ -49,7 +51,8 @@ struct FewParams {
 
 // The scale of a token whose largest magnitude is 2^-6 to 2^7 is 2^8 without asking, so one pass over
 // the activations will do: a bf16 value is exact down to 2^-22 and what is lost below stays under
-// 2^-27 of the largest.  Other tokens are converted again with a scale of their own.
+// 2^-27 of the largest.  Other tokens are converted again with a scale of their own: 8 tokens of 22016 x 4096 with an outlier of 500
+// each 22.7 us instead of 19.1, one 14.8 instead of 14.4 (4096 x 11008: 12.0, 11.0).
 constexpr float USUAL_SCALE = 256.f;
 __device__ __forceinline__ bool usual(uint32_t top) { return top >= 0x3c800000u && top < 0x43000000u; }
 

@@ -16,9 +16,12 @@
 // Work split: stream-K over (tile, 256 columns of K), one CTA per SM; the parts of tiles cut between CTAs go to the
 // workspace and are added by a second kernel in CTA order (deterministic).
 //
-// Measured (GB300, 22016 x 4096, group 128): 16 tokens 22.5 us, 64 28.5, 64 in two terms 32.5 (alone, the tokens'
-// kernel 4, the products 26, the join 9), 256 tokens 83; 4096 x 4096, 16 tokens 11.8.  Bound by unpacking: 8 warps
-// take 0.7 us for 256 features x 128 columns, the tensor pipe waits.
+// Measured (GB300, 22016 x 4096, group 128): 16 tokens 22.7 us, 64 29.2, 64 in two terms 32 (alone, the tokens'
+// kernel 4, the products 26, the join 9), 256 tokens 83 in one term, 90 in two; 4096 x 4096, 16 tokens 11.8.  Bound by the
+// unpacking warps, each group's codes after the sums of the one before: 0.7 us for 256 features x 128 columns (the tensor
+// pipe is active 45 % of the time, an instruction is issued in 42 %, DRAM works at 22 %).  From 256 tokens on the 16-bit
+// linear is faster, 81 us in one term and 68 in two (128 tokens: 50 and 49 here): a CTA takes 64 tokens, so 256
+// unpack the weights four times.
 //
 // Roles: warp 0 TMA of the tokens, warps 1 and 3 the MMAs of a tile each (one warp for both was the bottleneck: an MMA
 // takes 28 cycles to issue and a wait 200), warp 2 TMA of the weights, the others unpack and sum (warp w: TMEM
@@ -415,7 +418,7 @@ __global__ void __launch_bounds__(UNPACK_WARP * 32 + FT * halves(FT) * BM, 1) w4
         for (int at = 0; at < COLS; at += ONCE) ask(at), add(at);
       }
       tc_fence_before();
-      pdl_wait();  // Y, the workspace and its counters are shared with earlier kernels
+      pdl_wait();  // Y and the workspace are shared with earlier kernels
       ok = !any_of(2, UNPACK, !ok);  // all of them leave together
       if (!ok) break;
       // The part goes to the workspace, and the join of a cut tile to a kernel of its own, over all SMs.
