@@ -402,3 +402,28 @@ def test_linear_w4_extreme_activations_rounded(M, group, zeros):
     rest = [i for i in range(M) if i != 3]
     assert _rel_rows(Y[rest], ref[rest]) <= ROUNDED_TOL
     assert not torch.isfinite(Y[3]).all() and (Y[4] == 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", HIDDEN)
+@pytest.mark.parametrize("word", [0xffffffff, 0x7f807f80, 0x7e007e00], ids=["nan", "inf", "large"])
+def test_weight_sums_of_rows_that_no_counted_query_sees(case, word):
+    # local rows without numbers draw nothing from queries that do not see them, and change no other row's sum
+    ctx, G, H, hd, nq, n_local = case
+    g, r = _gen(83, len(ctx), G, nq), np.random.default_rng(83)
+    cache = Cache(g, [n + n_local for n in ctx], G, hd)
+    masks = _masks("tree", n_local, r)
+    q = _normal(g, len(ctx) * nq, H * hd)
+    bad = sorted({n_local - 1, n_local // 2} - {0})
+    counts = torch.tensor([float(not any(masks[i] >> j & 1 for j in bad)) for i in range(nq)], device="cuda").repeat(len(ctx))
+    scores = torch.rand(len(ctx), G, cache.pages * 16, generator=g, device="cuda")
+    want, lse = scores.double(), torch.zeros(len(ctx) * nq, H, device="cuda")
+    for b, z in enumerate(_probabilities(cache, q, ctx, masks, nq, 0, n_local, H, nq)):
+        lse[b * nq:(b + 1) * nq] = torch.logsumexp(z, -1).T.float()
+        p = torch.exp(z - lse[b * nq:(b + 1) * nq].T[:, :, None].double()).nan_to_num(0.0) * counts[:nq, None].double()
+        want[b, :, :ctx[b] + n_local] += p.view(G, H // G * nq, -1).sum(1)
+        for j in bad:
+            _spoil(cache, b, ctx[b] + j, word)
+    pkg.op_kv4_score(q, lse, cache.pool, cache.table, _ints(ctx), _anc(masks), scores, nq, 0, n_local, nq, H, hd, weight=counts)
+    pkg.op_sync()
+    assert _rel_rows(scores, want) <= ATT_TOL
